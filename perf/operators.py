@@ -278,7 +278,7 @@ def _handle(s):
                 n_blocks=s["blocks"], n_q_heads=c["q_heads"], n_kv_heads=c["kv_heads"], page_size=c["page"], kv_dtype=_dtype(c),
                 sink_pages=c["sink"], recent_pages=c["recent"],
                 buffers={n: s[n] for n in ("pages", "exps", "means", "mean_scales") if n in s})
-            s["ws"] = s["cache"].workspace(s["rows"])
+            s["ws"] = s["cache"].workspace(s["rows"], select=c["op"] == "select")
     return s["rows"], s.get("cache")
 
 
