@@ -459,6 +459,119 @@ int kvd_bind_tier(kvd_ctx* ctx, kvd_tier* tier);
  * its directory had already been updated for pages that did not arrive. */
 int kvd_step_tiered(kvd_ctx* ctx, int32_t layer, int32_t step, const void* q, float* out, float* lse, void* stream);
 
+/* ---- paged cache in 8 bits -------------------------------------------------------------------- */
+/*
+ * The K/V of requests that stay on the GPU, in half the bytes: one pool of blocks shared by all requests of a
+ * layer, a page table per request, keys and values in 8 bits with a scale for each page and head.  Four calls
+ * make a step: kvd_q8_map (once for all layers), then per layer kvd_q8_append, kvd_q8_select if the rows attend
+ * to selected pages only, and kvd_q8_attn.  They need no kvd_ctx and keep nothing from one call to the next:
+ * every pointer below is device memory of the caller's, the two structs are host memory read during the call.
+ * Nothing is allocated and no decision is taken on the host from device data, so a step can be captured into a
+ * HIP graph and replayed while the requests grow inside the sizes it was captured with.
+ *
+ * Sizes: P tokens a page, a multiple of 16 up to 256; D = 128; G = Hq / Hkv <= 8; Hkv <= 256; NB blocks;
+ * B sequences <= 4096; NP = max_pages <= 65536 pages a sequence; T = n_rows <= 131072 rows a step.  A *row* is one new
+ * token of one sequence; the rows of a sequence are consecutive, and the sequences follow each other in order.
+ *
+ * Values.  A page's keys (and, apart from them, its values) of one head share a scale 2^e: a stored code c of type
+ * e4m3 (OCP: no infinities, largest 448) stands for c * 2^e, e in -96..120.  Powers of two lose nothing when a scale
+ * grows, and quantisation by them is exact arithmetic.
+ *
+ * Layout.  pages: [NB][Hkv][P/16] tiles of 16 tokens, 4096 bytes each: 2048 bytes of keys, then 2048 of values, in the
+ * order in which a wave's lanes take them into matrix operands.  Key of token t, element d of a tile:
+ *   byte (d/64)*1024 + ((d/8%4)*16 + t)*16 + (d/32%2)*8 + d%8;
+ * value:
+ *   byte 2048 + (d/64)*1024 + ((t/4)*16 + d%16)*16 + (d/16%4)*4 + t%4.
+ *
+ * Bad input on the device.  A block number outside 0..NB-1 is never followed: kvd_q8_append leaves such a run out,
+ * kvd_q8_select scores the page as -infinity, and kvd_q8_attn treats the page's tokens as not visible.  Runs that leave their
+ * page or the rows, rows of a sequence outside 0..B-1 and positions outside 0..NP*P-1 are left out.
+ *
+ * Alignment: q, k_new, v_new, out, pages, means and workspace start on 16 bytes; row strides are in elements, at least a
+ * row long and multiples of 8.  Everything else is aligned to its type.  Buffers must not overlap unless a call says so.
+ */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads;
+  int32_t head_dim;        /* 128 */
+  int32_t page_size;       /* P */
+  int32_t n_blocks;        /* NB */
+  int32_t sink_pages;      /* kvd_q8_select: first and last visible pages of a row that are always selected, */
+  int32_t recent_pages;    /* counted inside k */
+  int32_t kv_dtype;        /* kvd_dtype: type of q, k_new, v_new and out */
+  float softmax_scale;     /* 0 means 1/sqrt(D) */
+  void* pages;             /* [NB][Hkv][P/16][4096] bytes */
+  int8_t* exps;            /* [NB][Hkv][2]: e of the keys, e of the values; starts on 2 bytes */
+  int8_t* means;           /* [NB][Hkv][D]: the page's mean key is means * mean_scales */
+  float* mean_scales;      /* [NB][Hkv] */
+} kvd_q8_cache;
+
+/* A step's rows.  Written by kvd_q8_map and read by the other calls; a caller may also fill them itself. */
+typedef struct {
+  int32_t n_seqs;          /* B */
+  int32_t max_pages;       /* NP */
+  int32_t n_rows;          /* T: rows that the buffers hold; a step may have fewer */
+  int32_t max_runs;        /* R: runs that the buffer holds, <= 131072 */
+  int32_t page_size;       /* P */
+  int32_t n_blocks;        /* NB */
+  int32_t* page_table;     /* [B][NP] block of each page */
+  int32_t* kv_len;         /* [B] tokens with this step's */
+  int32_t* row_start;      /* [B+1] first row of each sequence, and the number of rows */
+  int32_t* row_seq;        /* [T] sequence of each row, -1 behind the last */
+  int32_t* row_pos;        /* [T] position of the row's token in its sequence, -1 behind the last */
+  int32_t* runs;           /* [R][4], 16-byte aligned: the new tokens of one page: block, first row, offset of the first
+                              in the page, number; block -1 behind the last.  No block twice in one step. */
+  int32_t* counts;         /* [5]: rows, runs, blocks taken, blocks left free, and why nothing was mapped: 0, or the sum
+                              of 1 too few free blocks, 2 more than T rows, 4 more than R runs, 8 a length below zero or
+                              beyond NP * P */
+} kvd_q8_rows;
+
+/* Page tables and slot maps of a step from the requests' lengths.
+ *   seq_len [B] tokens cached so far;  n_new [B] tokens that the step adds, 0 and more
+ *   free_blocks [n_free] with *free_count (device) valid entries, taken from the last one down: first for the first
+ *   sequence, in page order.
+ * Writes the page-table entries of the pages that are begun (no others), and everything else in rows.  min(T, T/P + 2B)
+ * runs are always enough.  The inputs stay as they are: the caller takes counts[3] for the next step's free_count.  If the
+ * step does not fit, counts[4] says why, and it has no rows, no runs and no new blocks (kv_len = seq_len).
+ * A last page that is partly filled is continued in place: it must not be shared with another sequence. */
+int kvd_q8_map(const kvd_q8_rows* rows, const int32_t* seq_len, const int32_t* n_new, const int32_t* free_blocks,
+               int32_t n_free, const int32_t* free_count, void* stream);
+
+/* Quantises the step's keys and values into their pages, run by run and head by head.
+ *   k_new, v_new [T][Hkv][D] kv_dtype, rows k_stride and v_stride elements apart (heads D apart).
+ * With amax the largest finite magnitude of the run's new elements, need = the least e >= -96 with amax <= 448 * 2^e.  A run
+ * that begins its page sets e = need and the codes behind the run to 0; any other sets e to the larger of need and the page's e,
+ * and rounds the codes before the run to the new scale if that grew (codes behind it stay).  Rounding is to nearest, ties to
+ * even; an infinity becomes 448 * 2^e with its sign, a NaN becomes 0: the cache holds numbers only, so that no place that a
+ * mask hides can reach a result.  The index entry is that of all n tokens up to the run's end: with S_d the sum of their
+ * key codes times 2^9 (a whole number) and s the least shift >= 0 with max |S| <= 127 * 2^s, means = S / 2^s rounded to the
+ * nearest, ties to even, and mean_scales = 2^(s - 9 + e) / n in fp32. */
+int kvd_q8_append(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* k_new, int64_t k_stride,
+                  const void* v_new, int64_t v_stride, void* stream);
+
+/* Bytes of workspace that kvd_q8_attn (select == 0) or kvd_q8_select (select != 0) needs for these sizes; negative: a
+ * kvd_status.  Zero it once; every call leaves it ready for the next.  A call that runs, or a graph that is replayed, at the
+ * same time as another needs a workspace of its own. */
+int64_t kvd_q8_workspace_bytes(const kvd_q8_cache* cache, const kvd_q8_rows* rows, int32_t select);
+
+/* Selects pages for every row and KV head by a score in 8 bits.
+ *   q [T][Hq][D] kv_dtype, rows q_stride elements apart;  sel_pages [T][Hkv][k] int32 out, k <= 2048.
+ * The group's query heads are summed and rounded to whole numbers qi = rne(sum * (127 / max |sum|)) (fp64; 0 where that is not
+ * finite); score = fp32((qi . means) * mean_scales): the product is a whole number below 2^24, so that the score is rounded
+ * once and does not depend on any order of summation.  Of the pages that begin at or before the row's position, the first
+ * sink_pages and the last recent_pages are taken, then those with the best scores, ties to the lower page; ascending, -1
+ * behind the last.  sink_pages + recent_pages <= k (KVD_ERR_CAPACITY).  Rows without a sequence are left as they were. */
+int kvd_q8_select(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, int32_t* sel_pages,
+                  int32_t topk_pages, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Attention of every row over the tokens at and before its position: all of them (sel_pages NULL), or those in the pages
+ * that sel_pages [T][Hkv][k] names for the row and head, as kvd_q8_select writes them: each at most once, -1 behind the last.
+ *   q [T][Hq][D] kv_dtype, rows q_stride elements apart;  out [T][Hq][D] kv_dtype;  lse [T][Hq] fp32 or NULL.
+ * out = softmax(scale * q K^T) V, lse = log sum exp of the scaled logits; 0 and -infinity where a row sees nothing.  Sums,
+ * maxima and accumulators are fp32.  Rows without a sequence are left as they were.  kv_len and row_start must be those of
+ * row_seq and row_pos. */
+int kvd_q8_attn(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, const int32_t* sel_pages,
+                int32_t topk_pages, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* ---- counters ------------------------------------------------------------------------------ */
 
 /* mode 0: off.

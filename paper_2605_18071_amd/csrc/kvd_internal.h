@@ -182,3 +182,6 @@ hipError_t kvd_run_build_centroids(kvd_ctx* c, int layer, int iterations, int32_
 hipError_t kvd_launch_append(kvd_ctx* c, int layer, const void* k_new, const void* v_new, hipStream_t s);
 hipError_t kvd_launch_advance(kvd_ctx* c, hipStream_t s);
 hipError_t kvd_launch_fill_i32(int32_t* p, int32_t v, size_t n, hipStream_t s);
+// Workspaces of the 8-bit paged cache's calls (kvd_q8_attn.hip, kvd_q8_select.hip); the structs have been checked
+int64_t kvd_q8_attn_bytes(const kvd_q8_cache* c, const kvd_q8_rows* r);
+int64_t kvd_q8_select_bytes(const kvd_q8_cache* c, const kvd_q8_rows* r);

@@ -1,0 +1,621 @@
+// Attention of a step's rows over the pages of the 8-bit cache.
+//
+// S^T = K Q^T and O^T += V^T P^T on the matrix cores, 32 tokens at a time: a result's columns are query rows (a row of the
+// step and a head of the group), and the softmaxed S^T of a lane is, register for register, its operand of the second
+// product.  Tiles come from memory in operand order, 16 bytes a lane and load; codes become 16-bit numbers in registers, which
+// holds every e4m3 value exactly.  The keys' scale goes into the logits, the values' into the conversion.
+//
+// One pass with a running maximum m and sum l of a column: p = 2^(x - m).  m is raised only when a logit passes it by
+// more than kSlack, so that the accumulators are rarely touched; p then stays below 2^kSlack, and nothing is lost, as all of this
+// is floating point.
+//
+// DUP (one row of up to 8 heads): the 16 columns hold each head twice, and the second copy takes what rounding P to
+// bf16 left of it: P is then 16 bits long at the price of nothing, as the columns would be empty.  Otherwise P is rounded to
+// the type of q, half a step of 2^-9 (bf16) or 2^-12 (f16) of each weight, like the output.
+#include "kvd_q8.h"
+
+namespace kvd {
+namespace q8 {
+
+constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
+constexpr int kAttnGroups = 512;               // workgroups of the dense form: two for each CU
+constexpr int kLeastTiles = 16;                // tiles of a workgroup at least
+constexpr int kCoopTiles = 8;                  // from so many tiles on a piece is shared by the workgroup's waves
+constexpr int kPartFloats = kHeadDim + 4;      // a column's partial result: accumulators, maximum, sum
+constexpr float kLowest = -3.0e38f, kSlack = 8.f;
+constexpr int kNowhere = 1 << 30;              // position of a tile that no row sees
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttnArgs {
+  const uint16_t* q;
+  long long q_stride;
+  const int32_t *table, *kv_len, *row_start, *row_seq, *row_pos, *sel;
+  const unsigned char* pages;
+  const int8_t* exps;
+  uint16_t* out;
+  float *lse, *part;
+  int32_t* ticket;
+  int B, NP, T, H, G, P, NB, k, R, W, S;       // R rows of a unit, W workgroups (dense), S splits of a unit (selected)
+  float scale_log2;
+};
+
+// What the rows of one unit (up to R rows of a sequence, one head) have in common
+struct Unit {
+  int row0, rows, h, seq, pos0, entries;       // pos0: position of row0; entries: pages (or selected pages)
+};
+
+template <bool BF16> struct Op { typedef bf16x8 type; };
+template <> struct Op<false> { typedef f16x8 type; };
+
+template <bool BF16>
+__device__ __forceinline__ f32x4 mfma32(typename Op<BF16>::type a, typename Op<BF16>::type b, f32x4 c) {
+  if constexpr (BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// Eight codes to an operand, times 2^e where scale is that
+template <bool BF16>
+__device__ __forceinline__ typename Op<BF16>::type widen(u32 lo, u32 hi, float s_lo, float s_hi) {
+  u32 w[4];
+  if constexpr (BF16) {
+    w[0] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s_lo, false));
+    w[1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s_lo, true));
+    w[2] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s_hi, false));
+    w[3] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s_hi, true));
+  } else {
+    w[0] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, s_lo, false));
+    w[1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, s_lo, true));
+    w[2] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, s_hi, false));
+    w[3] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, s_hi, true));
+  }
+  return __builtin_bit_cast(typename Op<BF16>::type, make_uint4(w[0], w[1], w[2], w[3]));
+}
+__device__ __forceinline__ u32 word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// Two tiles on their way
+struct Pair {
+  uint4 k[2][2], v[2][2];
+  int tok[2], ek[2], ev[2];
+};
+
+template <bool BF16, int NQ, bool DUP, bool SEL>
+struct Wave {
+  static constexpr bool kPBf16 = DUP || BF16;  // P and V in bf16
+  f32x4 o[NQ][8];
+  float m[NQ], l[NQ];
+  typename Op<BF16>::type q[NQ][4];
+  int lim[NQ];                                 // last position that the lane's column sees
+  int vref;                                    // f16 values: accumulators hold 2^-vref of the result's numerator
+
+  const AttnArgs& a;
+  const int lane, c, n;
+  Unit u;
+  // the 64 page entries at hand: block and exponents of entry e0 + lane
+  int e0, e, sub, t, t1, blk, ex, pg;
+
+  __device__ __forceinline__ Wave(const AttnArgs& a_) : a(a_), lane(threadIdx.x % kWave), c((threadIdx.x % kWave) >> 4), n(threadIdx.x & 15) {}
+
+  // Row of the unit and head of the group of column n + 16 g
+  __device__ __forceinline__ void column(int g, int& r, int& head) const {
+    if (DUP) { r = 0; head = n & 7; }
+    else { const int col = n + 16 * g; r = col / a.G; head = col - r * a.G; }
+  }
+  __device__ __forceinline__ bool real(int r, int head) const { return head < a.G && r < u.rows; }
+
+  __device__ __forceinline__ void begin(const Unit& unit) {
+    u = unit;
+    vref = -1000;
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+      int r, head;
+      column(g, r, head);
+      const bool ok = real(r, head);
+      lim[g] = ok ? u.pos0 + r : -1;
+      const uint16_t* src = a.q + (long long)(u.row0 + r) * a.q_stride + (u.h * a.G + head) * kHeadDim + c * 8;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (ok) x = *reinterpret_cast<const uint4*>(src + j * 32);
+        q[g][j] = __builtin_bit_cast(typename Op<BF16>::type, x);
+      }
+      m[g] = kLowest;
+      l[g] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  __device__ __forceinline__ void fetch_entries() {
+    const int i = e0 + lane;
+    blk = -1;
+    pg = 0;
+    ex = 0;
+    if (i < u.entries) {
+      pg = SEL ? a.sel[((size_t)u.row0 * a.H + u.h) * a.k + i] : i;
+      if ((unsigned)pg < (unsigned)a.NP) blk = a.table[(size_t)u.seq * a.NP + pg];
+      if ((unsigned)blk >= (unsigned)a.NB) blk = -1;
+      if (blk >= 0) ex = *reinterpret_cast<const int16_t*>(a.exps + ((size_t)blk * a.H + u.h) * 2);
+    }
+  }
+  __device__ __forceinline__ void load(Pair& p) {
+    const int tpp = a.P / kTile;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int b = -1;
+      if (t < t1) {
+        if (e - e0 == kWave) { e0 = e; fetch_entries(); }
+        b = __builtin_amdgcn_readlane(blk, e - e0);
+        const int x = __builtin_amdgcn_readlane(ex, e - e0);
+        p.ek[i] = (int8_t)x;
+        p.ev[i] = (int8_t)(x >> 8);
+        p.tok[i] = __builtin_amdgcn_readlane(pg, e - e0) * a.P + sub * kTile;
+      }
+      if (b >= 0) {
+        const unsigned char* at = a.pages + (((size_t)b * a.H + u.h) * tpp + sub) * kTileBytes + lane * 16;
+        p.k[i][0] = load_stream16(at);
+        p.k[i][1] = load_stream16(at + 1024);
+        p.v[i][0] = load_stream16(at + 2048);
+        p.v[i][1] = load_stream16(at + 3072);
+      } else {
+        p.tok[i] = kNowhere;
+        p.ek[i] = p.ev[i] = kExpMin;
+        p.k[i][0] = p.k[i][1] = p.v[i][0] = p.v[i][1] = make_uint4(0, 0, 0, 0);
+      }
+      ++t;
+      if (++sub == tpp) { sub = 0; ++e; }
+    }
+  }
+
+  __device__ __forceinline__ void take(const Pair& p) {
+    f32x4 s[NQ][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) s[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const auto k = widen<BF16>(word(p.k[i][j >> 1], (j & 1) * 2), word(p.k[i][j >> 1], (j & 1) * 2 + 1), 1.f, 1.f);
+#pragma unroll
+        for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(k, q[g][j], s[g][i]);
+      }
+    }
+    const float ks[2] = {a.scale_log2 * two_to(p.ek[0]), a.scale_log2 * two_to(p.ek[1])};
+    float f[2] = {1.f, 1.f};
+    if (!kPBf16) {                             // f16: weights times 2^(ev - vref), at most 2^kSlack
+      const int top = max(p.ev[0], p.ev[1]);
+      if (top > vref) {
+        const float down = two_to(max(vref - top, -126));
+#pragma unroll
+        for (int g = 0; g < NQ; ++g)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[g][i] *= down;
+        vref = top;
+      }
+      f[0] = two_to(max(p.ev[0] - vref, -126));
+      f[1] = two_to(max(p.ev[1] - vref, -126));
+    }
+    uint4 w[NQ];
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = s[g][i >> 2][i & 3] * ks[i >> 2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (p.tok[i] + kTile - 1 > u.pos0) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (p.tok[i] + c * 4 + y > lim[g]) x[i * 4 + y] = -INFINITY;
+        }
+      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(mx > m[g] + kSlack)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        // (a column that does not need it stays, so that no row's result depends on its neighbours)
+        const float to = mx > m[g] + kSlack ? mx : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
+        m[g] = to;
+        l[g] *= down;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[g][i] *= down;
+      }
+      float pr[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(x[i] - m[g]);
+      l[g] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+      u32 ww[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float p0 = pr[2 * i], p1 = pr[2 * i + 1];
+        if (!kPBf16) { p0 *= f[i >> 1]; p1 *= f[i >> 1]; }
+        ww[i] = pack2<kPBf16>(p0, p1);
+        if (DUP) {
+          const u32 rest = pack2<true>(p0 - as_f32(ww[i] << 16), p1 - as_f32(ww[i] & 0xffff0000u));
+          ww[i] = n & 8 ? rest : ww[i];
+        }
+      }
+      w[g] = make_uint4(ww[0], ww[1], ww[2], ww[3]);
+    }
+    const float v0 = kPBf16 ? two_to(p.ev[0]) : 1.f, v1 = kPBf16 ? two_to(p.ev[1]) : 1.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const auto v = widen<kPBf16>(word(p.v[0][i >> 2], i & 3), word(p.v[1][i >> 2], i & 3), v0, v1);
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) o[g][i] = mfma32<kPBf16>(v, __builtin_bit_cast(typename Op<kPBf16>::type, w[g]), o[g][i]);
+    }
+  }
+
+  // Tiles [from, to) of the unit
+  __device__ __forceinline__ void sweep(int from, int to) {
+    if (from < to) {
+      const int tpp = a.P / kTile;
+      t = from; t1 = to;
+      e = from / tpp;
+      sub = from - e * tpp;
+      e0 = e;
+      fetch_entries();
+      Pair p[2];
+      load(p[0]);
+      for (int left = to - from; left > 0; left -= 4) {
+        load(p[1]);
+        take(p[0]);
+        if (left <= 2) break;
+        load(p[0]);
+        take(p[1]);
+      }
+    }
+    // a column's four lanes have a quarter of its sum each
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+      l[g] += __shfl_xor(l[g], 16, kWave);
+      l[g] += __shfl_xor(l[g], 32, kWave);
+      if (!kPBf16) {
+        const float up = vref > -1000 ? two_to(vref) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[g][i] *= up;
+      }
+      if (DUP)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) o[g][i][y] += __shfl_xor(o[g][i][y], 8, kWave);
+    }
+  }
+};
+
+// A column's result over all tokens
+template <bool BF16, int N>
+__device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, int head, int d, const float (&v)[N], float m, float l) {
+  const size_t at = (size_t)(u.row0 + r) * a.H * a.G + u.h * a.G + head;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  u32 w[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) w[i] = pack2<BF16>(l == 0.f ? 0.f : v[2 * i] * inv, l == 0.f ? 0.f : v[2 * i + 1] * inv);
+  if constexpr (N == 8) *reinterpret_cast<uint4*>(a.out + at * kHeadDim + d) = make_uint4(w[0], w[1], w[2], w[3]);
+  else *reinterpret_cast<uint2*>(a.out + at * kHeadDim + d) = make_uint2(w[0], w[1]);
+  if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// Joins the `count` partial results of a unit; slot(i) is the i-th one's number.  By the threads tid, tid + nt, ...
+template <bool BF16, int COLS, bool DUP, class Slot>
+__device__ __forceinline__ void join(const AttnArgs& a, const Unit& u, int count, Slot slot, int tid, int nt) {
+  const int cols = DUP ? a.G : u.rows * a.G;
+  for (int x = tid; x < cols * 16; x += nt) {
+    const int col = x >> 4, d = (x & 15) * 8;
+    float M = kLowest;
+    for (int i = 0; i < count; ++i) {
+      const float* p = a.part + ((size_t)slot(i) * COLS + col) * kPartFloats + kHeadDim;
+      if (load_agent(p + 1) != 0.f) M = fmaxf(M, load_agent(p));
+    }
+    float L = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < count; ++i) {
+      const float* p = a.part + ((size_t)slot(i) * COLS + col) * kPartFloats;
+      const float l = load_agent(p + kHeadDim + 1);
+      if (l == 0.f) continue;                  // (nothing visible there, and no accumulators)
+      const float f = __builtin_amdgcn_exp2f(load_agent(p + kHeadDim) - M);
+      L += l * f;
+#pragma unroll
+      for (int y = 0; y < 8; ++y) v[y] += load_agent(p + d + y) * f;
+    }
+    emit<BF16>(a, u, col / a.G, col % a.G, d, v, M, L);
+  }
+}
+
+// Where a piece's result goes: to the output if it is all of the unit (count == 1), else to slot `mine` of the partial
+// results, which the last of the `count` pieces to arrive joins.
+template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
+__device__ __forceinline__ void finish_wave(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, int count, int mine, int ticket, Slot slot) {
+  constexpr int COLS = DUP ? 8 : 16 * NQ;
+#pragma unroll
+  for (int g = 0; g < NQ; ++g) {
+    int r, head;
+    w.column(g, r, head);
+    if (!w.real(r, head) || (DUP && (w.n & 8))) continue;
+    if (count == 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v[4] = {w.o[g][i][0], w.o[g][i][1], w.o[g][i][2], w.o[g][i][3]};
+        emit<BF16>(a, w.u, r, head, i * 16 + w.c * 4, v, w.m[g], w.l[g]);
+      }
+    } else {
+      float* p = a.part + ((size_t)mine * COLS + r * a.G + head) * kPartFloats;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) store_agent(p + i * 16 + w.c * 4 + y, w.o[g][i][y]);
+      if (w.c == 0) { store_agent(p + kHeadDim, w.m[g]); store_agent(p + kHeadDim + 1, w.l[g]); }
+    }
+  }
+  if (count == 1) return;
+  wave_drain_memory();
+  int before = 0;
+  if (w.lane == 0) before = __hip_atomic_fetch_add(a.ticket + ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  before = __builtin_amdgcn_readfirstlane(before);
+  if (before != count - 1) return;
+  if (w.lane == 0) store_agent(a.ticket + ticket, 0);
+  join<BF16, COLS, DUP>(a, w.u, count, slot, w.lane, kWave);
+}
+
+template <int NQ>
+struct AttnLds {
+  float ml[kAttnWaves][16 * NQ][2];
+  __align__(16) float o[kAttnWaves][16][kPartFloats];
+  int last;
+};
+
+// The same for a piece that the waves of the workgroup shared
+template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
+__device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, int count, int mine,
+                                             int ticket, Slot slot) {
+  constexpr int COLS = DUP ? 8 : 16 * NQ;
+  const int tid = threadIdx.x, wave = tid / kWave;
+  __syncthreads();                             // (earlier pieces have been read)
+#pragma unroll
+  for (int g = 0; g < NQ; ++g)
+    if (w.c == 0) {
+      lds.ml[wave][g * 16 + w.n][0] = w.l[g] == 0.f ? kLowest : w.m[g];
+      lds.ml[wave][g * 16 + w.n][1] = w.l[g];
+    }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < NQ; ++g) {
+    float M = kLowest;
+#pragma unroll
+    for (int i = 0; i < kAttnWaves; ++i) M = fmaxf(M, lds.ml[i][g * 16 + w.n][0]);
+    const float f = w.l[g] == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.m[g] - M);
+    if (g > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<f32x4*>(&lds.o[wave][w.n][i * 16 + w.c * 4]) = w.o[g][i] * f;
+    __syncthreads();
+    const int n = tid >> 4, d = (tid & 15) * 8;   // a column and eight of its elements
+    const int col = g * 16 + n;
+    int r = 0, head = n;
+    if (!DUP) { r = col / a.G; head = col - r * a.G; }
+    if (w.real(r, head) && !(DUP && n >= 8)) {
+      float top = kLowest, L = 0.f, v[8];
+#pragma unroll
+      for (int i = 0; i < kAttnWaves; ++i) top = fmaxf(top, lds.ml[i][col][0]);
+#pragma unroll
+      for (int i = 0; i < kAttnWaves; ++i) {
+        const float l = lds.ml[i][col][1];
+        if (l != 0.f) L += l * __builtin_amdgcn_exp2f(lds.ml[i][col][0] - top);
+      }
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        v[y] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kAttnWaves; ++i) v[y] += lds.o[i][n][d + y];
+      }
+      if (count == 1) emit<BF16>(a, w.u, r, head, d, v, top, L);
+      else {
+        float* p = a.part + ((size_t)mine * COLS + r * a.G + head) * kPartFloats;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) store_agent(p + d + y, v[y]);
+        if (d == 0) { store_agent(p + kHeadDim, top); store_agent(p + kHeadDim + 1, L); }
+      }
+    }
+  }
+  if (count == 1) return;
+  wave_drain_memory();
+  __syncthreads();
+  if (tid == 0) {
+    lds.last = __hip_atomic_fetch_add(a.ticket + ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == count - 1;
+    if (lds.last) store_agent(a.ticket + ticket, 0);
+  }
+  __syncthreads();
+  if (lds.last) join<BF16, COLS, DUP>(a, w.u, count, slot, tid, kAttnThreads);
+}
+
+// Tiles [t0, t1) of a unit: by all waves, or, a short piece, by wave `solo` alone.
+template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
+__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, const Unit& u, int t0, int t1,
+                                      int solo, int count, int mine, int ticket, Slot slot) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (!SEL) t1 = min(t1, max(t0, (u.pos0 + u.rows - 1) / kTile + 1));   // none of the rows sees more
+  if (t1 - t0 < kCoopTiles) {
+    if (wave != solo) return;
+    w.begin(u);
+    w.sweep(t0, t1);
+    finish_wave(a, w, count, mine, ticket, slot);
+  } else {
+    const int per = ((t1 - t0 + 1) / 2 + kAttnWaves - 1) / kAttnWaves * 2;
+    w.begin(u);
+    w.sweep(min(t0 + wave * per, t1), min(t0 + (wave + 1) * per, t1));
+    finish_group(a, w, lds, count, mine, ticket, slot);
+  }
+}
+
+// All tokens.  The units' tiles, one unit behind the other, are dealt out evenly: workgroup i has tiles [i, i + 1) * chunk of
+// them all, wherever units begin and end in there, so that lengths of any kind keep all CUs busy to the end.
+template <bool BF16, int NQ, bool DUP>
+__global__ __launch_bounds__(kAttnThreads, NQ == 4 ? 1 : 2) void q8_attn_dense_kernel(AttnArgs a) {
+  __shared__ AttnLds<NQ> lds;
+  __shared__ u64 scan[kAttnWaves];
+  __shared__ u64 s_base;
+  __shared__ int s_seq;
+  const int tid = threadIdx.x, lane = tid % kWave, wv = tid / kWave;
+  auto of = [&](int b, int& row0, int& rows, int& len, int& tiles) {   // returns units a head
+    row0 = min(max(a.row_start[b], 0), a.T);
+    rows = min(max(a.row_start[b + 1], row0), a.T) - row0;
+    len = min(max(a.kv_len[b], 0), a.NP * a.P);
+    tiles = max((len + kTile - 1) / kTile, 1);
+    return (rows + a.R - 1) / a.R;
+  };
+  const int per = (a.B + kAttnThreads - 1) / kAttnThreads, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  u64 mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    int row0, rows, len, tiles;
+    const int units = of(b, row0, rows, len, tiles);
+    mine += (u64)units * a.H * tiles;
+  }
+  u64 upto = mine;
+#pragma unroll
+  for (int x = 1; x < kWave; x <<= 1) {
+    const u64 y = ((u64)__shfl_up((u32)(upto >> 32), x, kWave) << 32) | __shfl_up((u32)upto, x, kWave);
+    if (lane >= x) upto += y;
+  }
+  if (lane == kWave - 1) scan[wv] = upto;
+  __syncthreads();
+  u64 all = 0;
+#pragma unroll
+  for (int i = 0; i < kAttnWaves; ++i) {
+    if (i < wv) upto += scan[i];
+    all += scan[i];
+  }
+  u64 chunk = (all + a.W - 1) / a.W;
+  if (chunk < (u64)kLeastTiles) chunk = kLeastTiles;
+  const u64 lo = blockIdx.x * chunk, hi = min(lo + chunk, all);
+  if (lo >= all) return;
+  if (upto - mine <= lo && lo < upto) {
+    u64 base = upto - mine;
+    int b = b0;
+    for (; b < b1; ++b) {
+      int row0, rows, len, tiles;
+      const int units = of(b, row0, rows, len, tiles);
+      const u64 n = (u64)units * a.H * tiles;
+      if (lo < base + n) break;
+      base += n;
+    }
+    s_base = base;
+    s_seq = b;
+  }
+  __syncthreads();
+  Wave<BF16, NQ, DUP, false> w(a);
+  u64 at = lo, base = s_base;
+  int b = __builtin_amdgcn_readfirstlane(s_seq), solo = 0;
+  while (at < hi && b < a.B) {
+    int row0, rows, len, tiles;
+    const int units = of(b, row0, rows, len, tiles) * a.H;
+    const u64 end = base + (u64)units * tiles;
+    while (at < min(end, hi)) {
+      const u64 i = (at - base) / tiles, begin = base + i * tiles;
+      const int t0 = (int)(at - begin), t1 = (int)min((u64)tiles, hi - begin);
+      const int part = (int)(i / a.H);
+      Unit u;
+      u.seq = b;
+      u.h = (int)(i - (u64)part * a.H);
+      u.row0 = row0 + part * a.R;
+      u.rows = min(a.R, rows - part * a.R);
+      u.pos0 = len - rows + part * a.R;
+      u.entries = min((len + a.P - 1) / a.P, a.NP);
+      const int f = (int)(begin / chunk), count = (int)((begin + tiles - 1) / chunk) - f + 1;
+      // a workgroup has the beginning of one unit that goes on behind it, and at most one piece that began before it
+      piece(a, w, lds, u, t0, t1, solo, count, (int)blockIdx.x * 2 + (t0 == 0 ? 1 : 0), f,
+            [&](int x) { return x == 0 ? f * 2 + 1 : (f + x) * 2; });
+      solo = (solo + 1) % kAttnWaves;
+      at = begin + t1;
+    }
+    base = end;
+    ++b;
+  }
+}
+
+// Selected pages: a unit is one row and head, in S pieces.
+template <bool BF16>
+__global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_selected_kernel(AttnArgs a) {
+  __shared__ AttnLds<1> lds;
+  const int unit = blockIdx.x / a.S, s = blockIdx.x - unit * a.S;
+  Unit u;
+  u.row0 = unit / a.H;
+  u.h = unit - u.row0 * a.H;
+  u.rows = 1;
+  u.seq = a.row_seq[u.row0];
+  u.pos0 = a.row_pos[u.row0];
+  if ((unsigned)u.seq >= (unsigned)a.B || u.pos0 < 0 || u.pos0 >= a.NP * a.P) return;
+  u.entries = min(a.k, u.pos0 / a.P + 1);
+  const int tiles = u.entries * (a.P / kTile), per = (tiles + a.S - 1) / a.S;
+  Wave<BF16, 1, true, true> w(a);
+  piece(a, w, lds, u, min(s * per, tiles), min((s + 1) * per, tiles), 0, a.S, (int)blockIdx.x, unit,
+        [&](int x) { return unit * a.S + x; });
+}
+
+// Columns of a unit's products in 16s: as many rows as a sequence has on the average, 64 columns at most
+static int column_groups(int T, int B, int G) {
+  const int want = (int)((T + B - 1) / B) * G;
+  return want <= 16 ? 1 : want <= 32 ? 2 : 4;
+}
+
+}  // namespace q8
+}  // namespace kvd
+
+int64_t kvd_q8_attn_bytes(const kvd_q8_cache* c, const kvd_q8_rows* r) {
+  using namespace kvd::q8;
+  const int cols = r->n_rows <= r->n_seqs ? 8 : 16 * column_groups(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
+  return (int64_t)kAttnGroups * 4 + (int64_t)2 * kAttnGroups * cols * kPartFloats * 4;
+}
+
+extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const void* q, int64_t q_stride, const int32_t* sel_pages,
+                           int32_t topk_pages, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  using namespace kvd::q8;
+  using kvd::kHeadDim;
+  if (int e = check_cache(c, r)) return e;
+  if (!stride_ok(q_stride, c->n_q_heads)) return KVD_ERR_SHAPE;
+  if (sel_pages != nullptr && (topk_pages < 1 || topk_pages > KVD_MAX_TOPK)) return KVD_ERR_SHAPE;
+  if (!aligned(c->pages, 16) || !aligned(c->exps, 2) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return KVD_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(lse) & 3) || (reinterpret_cast<uintptr_t>(sel_pages) & 3)) return KVD_ERR_ARG;
+  if (!aligned(r->page_table, 4) || !aligned(r->kv_len, 4) || !aligned(r->row_start, 4) || !aligned(r->row_seq, 4) || !aligned(r->row_pos, 4)) return KVD_ERR_ARG;
+  if (workspace_bytes < kvd_q8_attn_bytes(c, r)) return KVD_ERR_CAPACITY;
+  kvd::q8::AttnArgs a;
+  a.q = static_cast<const uint16_t*>(q); a.q_stride = q_stride;
+  a.table = r->page_table; a.kv_len = r->kv_len; a.row_start = r->row_start; a.row_seq = r->row_seq; a.row_pos = r->row_pos;
+  a.sel = sel_pages;
+  a.pages = static_cast<const unsigned char*>(c->pages); a.exps = c->exps;
+  a.out = static_cast<uint16_t*>(out); a.lse = lse;
+  a.ticket = static_cast<int32_t*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAttnGroups * 4);
+  a.B = r->n_seqs; a.NP = r->max_pages; a.T = r->n_rows; a.H = c->n_kv_heads; a.G = c->n_q_heads / c->n_kv_heads;
+  a.P = c->page_size; a.NB = c->n_blocks; a.k = topk_pages;
+  a.W = kAttnGroups;
+  a.scale_log2 = (c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool bf16 = c->kv_dtype == KVD_BF16;
+  if (sel_pages != nullptr) {
+    const int64_t units = (int64_t)a.T * a.H;
+    const int tiles = topk_pages * (a.P / kTile);
+    int S = (int)(kAttnGroups / units);
+    if (S > tiles / kLeastTiles) S = tiles / kLeastTiles;
+    a.S = S < 1 ? 1 : S;
+    a.R = 1;
+    const dim3 grid((unsigned)(units * a.S));
+    if (bf16) hipLaunchKernelGGL(q8_attn_selected_kernel<true>, grid, dim3(kAttnThreads), 0, s, a);
+    else hipLaunchKernelGGL(q8_attn_selected_kernel<false>, grid, dim3(kAttnThreads), 0, s, a);
+    return launched();
+  }
+  a.S = 1;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(kAttnGroups), dim3(kAttnThreads), 0, s, a); };
+  if (a.T <= a.B) {
+    a.R = 1;
+    if (bf16) go(q8_attn_dense_kernel<true, 1, true>); else go(q8_attn_dense_kernel<false, 1, true>);
+    return launched();
+  }
+  const int groups = column_groups(a.T, a.B, a.G);
+  a.R = 16 * groups / a.G;
+  if (bf16) {
+    if (groups == 1) go(q8_attn_dense_kernel<true, 1, false>);
+    else if (groups == 2) go(q8_attn_dense_kernel<true, 2, false>);
+    else go(q8_attn_dense_kernel<true, 4, false>);
+  } else {
+    if (groups == 1) go(q8_attn_dense_kernel<false, 1, false>);
+    else if (groups == 2) go(q8_attn_dense_kernel<false, 2, false>);
+    else go(q8_attn_dense_kernel<false, 4, false>);
+  }
+  return launched();
+}

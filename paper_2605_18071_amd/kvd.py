@@ -59,6 +59,24 @@ class KvdStats(C.Structure):
     ]
 
 
+class KvdQ8Cache(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+        ("n_blocks", C.c_int32), ("sink_pages", C.c_int32), ("recent_pages", C.c_int32), ("kv_dtype", C.c_int32),
+        ("softmax_scale", C.c_float), ("pages", C.c_void_p), ("exps", C.c_void_p), ("means", C.c_void_p),
+        ("mean_scales", C.c_void_p),
+    ]
+
+
+class KvdQ8Rows(C.Structure):
+    _fields_ = [
+        ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("n_rows", C.c_int32), ("max_runs", C.c_int32),
+        ("page_size", C.c_int32), ("n_blocks", C.c_int32), ("page_table", C.c_void_p), ("kv_len", C.c_void_p),
+        ("row_start", C.c_void_p), ("row_seq", C.c_void_p), ("row_pos", C.c_void_p), ("runs", C.c_void_p),
+        ("counts", C.c_void_p),
+    ]
+
+
 EXPORTS = [
     "kvd_create", "kvd_destroy", "kvd_strerror", "kvd_last_hip_error", "kvd_abi_version",
     "kvd_bind_summaries", "kvd_bind_host_store", "kvd_bind_slot_pool", "kvd_set_seq_lens",
@@ -70,6 +88,7 @@ EXPORTS = [
     "kvd_tier_reset_stats", "kvd_tier_sequential_read_gbps", "kvd_layout_from_clusters", "kvd_bind_tier",
     "kvd_step_tiered", "kvd_step_layers", "kvd_sparse_decode_attn_noalloc",
     "kvd_set_step_shape", "kvd_get_step_shape", "kvd_calibrate_step_shape",
+    "kvd_q8_map", "kvd_q8_append", "kvd_q8_workspace_bytes", "kvd_q8_select", "kvd_q8_attn",
 ]
 
 _lib = None
@@ -136,12 +155,18 @@ def load() -> C.CDLL:
         "kvd_set_step_shape": [vp, i32, i32, i32, i32, i32],
         "kvd_get_step_shape": [vp, i32, i32p],
         "kvd_calibrate_step_shape": [vp, i32, i32, i32, vp, vp, vp, i32, i32p, f32p, f32p],
+        "kvd_q8_map": [vp, vp, vp, vp, i32, vp, vp],
+        "kvd_q8_append": [vp, vp, vp, C.c_int64, vp, C.c_int64, vp],
+        "kvd_q8_workspace_bytes": [vp, vp, i32],
+        "kvd_q8_select": [vp, vp, vp, C.c_int64, vp, i32, vp, C.c_int64, vp],
+        "kvd_q8_attn": [vp, vp, vp, C.c_int64, vp, i32, vp, vp, vp, C.c_int64, vp],
         "kvd_sparse_decode_attn_noalloc": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, C.c_float, i32, vp],
     }
     for name, args in protos.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = C.c_int
+    lib.kvd_q8_workspace_bytes.restype = C.c_int64
     lib.kvd_strerror.argtypes = [C.c_int]
     lib.kvd_strerror.restype = C.c_char_p
     _lib = lib
@@ -494,3 +519,158 @@ class KvdTier:
         g = C.c_double()
         self._check(self.lib.kvd_tier_sequential_read_gbps(self.handle, C.byref(g)), "kvd_tier_sequential_read_gbps")
         return g.value
+
+
+# ---- paged cache in 8 bits
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _buffer(name: str, t: torch.Tensor, shape, dtype, device) -> torch.Tensor:
+    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.is_contiguous() and t.device == device,
+          f"{name}: a contiguous {dtype} tensor of {tuple(shape)} on {device} is wanted, "
+          f"got {t.dtype} of {tuple(t.shape)} on {t.device}")
+    return t
+
+
+class _OnDevice:
+    """Calls into the library with the tensors' GPU current, on `stream` or that GPU's current stream."""
+
+    def _call(self, name: str, stream, *args):
+        index = self.device.index
+        _need(self.device.type == "cuda", f"{name}: tensors on a GPU are wanted, got {self.device}")
+        if stream is not None:
+            _need(stream.device == self.device, f"{name}: the stream is on {stream.device}, the tensors on {self.device}")
+        if torch.cuda.current_device() == index:
+            st = getattr(self.lib, name)(*args, _stream_handle(stream))
+        else:
+            with torch.cuda.device(index):
+                st = getattr(self.lib, name)(*args, _stream_handle(stream))
+        if st != OK:
+            raise KvdError(st, name)
+
+
+def _cuda(device) -> torch.device:
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
+
+
+class Q8Rows(_OnDevice):
+    """One kvd_q8_rows: the rows of a step of page_table's sequences, for at most `n_rows` rows.  Buffers that are not given
+    are made, without any rows in them."""
+
+    def __init__(self, page_table: torch.Tensor, *, page_size: int, n_blocks: int, n_rows: int, max_runs: Optional[int] = None,
+                 kv_len=None, row_start=None, row_seq=None, row_pos=None, runs=None, counts=None):
+        self.lib = load()
+        self.device = dev = page_table.device
+        _need(page_table.dim() == 2, "page_table: [sequences][pages] is wanted")
+        B, NP = page_table.shape
+        if max_runs is None:
+            max_runs = min(n_rows, n_rows // page_size + 2 * B)
+        self.n_seqs, self.n_rows, self.max_runs, self.page_size, self.n_blocks = B, n_rows, max_runs, page_size, n_blocks
+
+        def made(name, t, shape, fill):
+            if t is None:
+                return torch.full(shape, fill, dtype=torch.int32, device=dev)
+            return _buffer(name, t, shape, torch.int32, dev)
+
+        self.page_table = _buffer("page_table", page_table, (B, NP), torch.int32, dev)
+        self.kv_len = made("kv_len", kv_len, (B,), 0)
+        self.row_start = made("row_start", row_start, (B + 1,), 0)
+        self.row_seq = made("row_seq", row_seq, (n_rows,), -1)
+        self.row_pos = made("row_pos", row_pos, (n_rows,), -1)
+        self.runs = made("runs", runs, (max_runs, 4), -1)
+        self.counts = made("counts", counts, (5,), 0)
+        self.c = KvdQ8Rows(B, NP, n_rows, max_runs, page_size, n_blocks, self.page_table.data_ptr(), self.kv_len.data_ptr(),
+                           self.row_start.data_ptr(), self.row_seq.data_ptr(), self.row_pos.data_ptr(), self.runs.data_ptr(),
+                           self.counts.data_ptr())
+        self._ref = C.byref(self.c)
+
+    def map(self, seq_len: torch.Tensor, n_new: torch.Tensor, free_blocks: torch.Tensor, free_count: torch.Tensor, stream=None):
+        """kvd_q8_map: the step that adds n_new tokens to sequences of seq_len."""
+        _buffer("seq_len", seq_len, (self.n_seqs,), torch.int32, self.device)
+        _buffer("n_new", n_new, (self.n_seqs,), torch.int32, self.device)
+        _buffer("free_blocks", free_blocks, (free_blocks.numel(),), torch.int32, self.device)
+        _buffer("free_count", free_count, (1,), torch.int32, self.device)
+        self._call("kvd_q8_map", stream, self._ref, seq_len.data_ptr(), n_new.data_ptr(), free_blocks.data_ptr(),
+                   free_blocks.numel(), free_count.data_ptr())
+
+
+class Q8Cache(_OnDevice):
+    """One kvd_q8_cache: the 8-bit pages of a layer, over `buffers` (a dict of pages, exps, means and mean_scales) where
+    given, otherwise over new ones."""
+
+    def __init__(self, *, n_blocks: int, n_q_heads: int, n_kv_heads: int, page_size: int, kv_dtype, head_dim: int = 128,
+                 softmax_scale: float = 0.0, sink_pages: int = 0, recent_pages: int = 0, device="cuda", buffers=None):
+        self.lib = load()
+        buffers = dict(buffers or {})
+        _need(not set(buffers) - {"pages", "exps", "means", "mean_scales"}, "buffers: pages, exps, means and mean_scales are wanted")
+        self.device = next(iter(buffers.values())).device if buffers else _cuda(device)
+        _need(page_size >= 16 and page_size % 16 == 0, "page_size: a multiple of 16 is wanted")
+        self.kv_dtype = {KVD_F16: torch.float16, KVD_BF16: torch.bfloat16}.get(kv_dtype, kv_dtype)
+        _need(self.kv_dtype in (torch.float16, torch.bfloat16), "kv_dtype: float16 or bfloat16 is wanted")
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
+        shapes = dict(pages=((n_blocks, n_kv_heads, page_size // 16, 2, 2048), torch.uint8),
+                      exps=((n_blocks, n_kv_heads, 2), torch.int8), means=((n_blocks, n_kv_heads, head_dim), torch.int8),
+                      mean_scales=((n_blocks, n_kv_heads), torch.float32))
+        for name, (shape, dtype) in shapes.items():
+            t = buffers.get(name)
+            t = torch.zeros(shape, dtype=dtype, device=self.device) if t is None else _buffer(name, t, shape, dtype, self.device)
+            setattr(self, name, t)
+        self.c = KvdQ8Cache(n_q_heads, n_kv_heads, head_dim, page_size, n_blocks, sink_pages, recent_pages,
+                            KVD_F16 if self.kv_dtype == torch.float16 else KVD_BF16, softmax_scale, self.pages.data_ptr(),
+                            self.exps.data_ptr(), self.means.data_ptr(), self.mean_scales.data_ptr())
+        self._ref = C.byref(self.c)
+
+    def workspace(self, rows: Q8Rows, select: bool = False) -> torch.Tensor:
+        """A new workspace for attend, or for select, of these rows.  Calls that overlap in time need one each."""
+        n = self.lib.kvd_q8_workspace_bytes(self._ref, rows._ref, 1 if select else 0)
+        if n < 0:
+            raise KvdError(int(n), "kvd_q8_workspace_bytes")
+        return torch.zeros((n + 15) // 16 * 4, dtype=torch.int32, device=self.device)
+
+    def _rowed(self, name: str, t: torch.Tensor, heads: int, n_rows: int) -> int:
+        """Stride of a [rows][heads][head_dim] tensor whose rows may lie apart."""
+        _need(t.shape == (n_rows, heads, self.head_dim) and t.dtype == self.kv_dtype and t.device == self.device
+              and t.stride(2) == 1 and t.stride(1) == self.head_dim,
+              f"{name}: a {self.kv_dtype} tensor of {(n_rows, heads, self.head_dim)} on {self.device} with whole rows is wanted, "
+              f"got {t.dtype} of {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+        return t.stride(0) if n_rows > 1 else heads * self.head_dim
+
+    def _check_rows(self, rows: Q8Rows, workspace: Optional[torch.Tensor] = None):
+        _need(rows.device == self.device, "the rows and the cache are on different devices")
+        if workspace is not None:
+            _need(workspace.device == self.device and workspace.is_contiguous(), "workspace: a contiguous tensor on the cache's device is wanted")
+
+    def append(self, rows: Q8Rows, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
+        """kvd_q8_append: the rows' keys and values [rows][kv heads][head_dim] into their pages."""
+        self._check_rows(rows)
+        ks = self._rowed("k_new", k_new, self.n_kv_heads, rows.n_rows)
+        vs = self._rowed("v_new", v_new, self.n_kv_heads, rows.n_rows)
+        self._call("kvd_q8_append", stream, self._ref, rows._ref, k_new.data_ptr(), ks, v_new.data_ptr(), vs)
+
+    def select(self, rows: Q8Rows, q: torch.Tensor, sel_pages: torch.Tensor, workspace: torch.Tensor, stream=None):
+        """kvd_q8_select: the best pages of every row and KV head into sel_pages [rows][kv heads][k]."""
+        self._check_rows(rows, workspace)
+        qs = self._rowed("q", q, self.n_q_heads, rows.n_rows)
+        k = sel_pages.shape[-1]
+        _buffer("sel_pages", sel_pages, (rows.n_rows, self.n_kv_heads, k), torch.int32, self.device)
+        self._call("kvd_q8_select", stream, self._ref, rows._ref, q.data_ptr(), qs, sel_pages.data_ptr(), k,
+                   workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+    def attend(self, rows: Q8Rows, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, lse: Optional[torch.Tensor] = None,
+               sel_pages: Optional[torch.Tensor] = None, stream=None):
+        """kvd_q8_attn: attention of the rows over all their tokens, or over those in sel_pages."""
+        self._check_rows(rows, workspace)
+        qs = self._rowed("q", q, self.n_q_heads, rows.n_rows)
+        _buffer("out", out, (rows.n_rows, self.n_q_heads, self.head_dim), self.kv_dtype, self.device)
+        if lse is not None:
+            _buffer("lse", lse, (rows.n_rows, self.n_q_heads), torch.float32, self.device)
+        k = 0
+        if sel_pages is not None:
+            k = sel_pages.shape[-1]
+            _buffer("sel_pages", sel_pages, (rows.n_rows, self.n_kv_heads, k), torch.int32, self.device)
+        self._call("kvd_q8_attn", stream, self._ref, rows._ref, q.data_ptr(), qs, _ptr(sel_pages), k, out.data_ptr(), _ptr(lse),
+                   workspace.data_ptr(), workspace.numel() * workspace.element_size())
