@@ -165,6 +165,64 @@ struct Wave {
     }
   }
 
+  // f16 values: weights are taken times 2^(ev - vref), at most 2^kSlack; vref follows the largest ev
+  __device__ __forceinline__ void weigh(const int (&ev)[2], float (&f)[2]) {
+    const int top = max(ev[0], ev[1]);
+    if (top > vref) {
+      const float down = two_to(max(vref - top, -126));
+#pragma unroll
+      for (int g = 0; g < NQ; ++g)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[g][i] *= down;
+      vref = top;
+    }
+    f[0] = two_to(max(ev[0] - vref, -126));
+    f[1] = two_to(max(ev[1] - vref, -126));
+  }
+
+  // The products q k of a column with the pair's tokens (four of each tile a lane) to weights, as the operand of the second
+  // product.  ks: what the products are taken times for logits in powers of two, f: the weights' factors (f16)
+  __device__ __forceinline__ uint4 soften(int g, const f32x4 (&s)[2], const int (&tok)[2], const float (&ks)[2], const float (&f)[2]) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (tok[i] + kTile - 1 > u.pos0) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (tok[i] + c * 4 + y > lim[g]) x[i * 4 + y] = -INFINITY;
+      }
+    // (ks > 0 keeps the order)
+    float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * ks[0], fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])) * ks[1]);
+    if (__any(mx > m[g] + kSlack)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      // (a column that does not need it stays, so that no row's result depends on its neighbours)
+      const float to = mx > m[g] + kSlack ? mx : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
+      m[g] = to;
+      l[g] *= down;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[g][i] *= down;
+    }
+    float pr[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], ks[i >> 2], -m[g]));
+    l[g] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+    u32 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float p0 = pr[2 * i], p1 = pr[2 * i + 1];
+      if (!kPBf16) { p0 *= f[i >> 1]; p1 *= f[i >> 1]; }
+      w[i] = pack2<kPBf16>(p0, p1);
+      if (DUP) {
+        const u32 rest = pack2<true>(p0 - as_f32(w[i] << 16), p1 - as_f32(w[i] & 0xffff0000u));
+        w[i] = n & 8 ? rest : w[i];
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+
   __device__ __forceinline__ void take(const Pair& p) {
     f32x4 s[NQ][2];
 #pragma unroll
@@ -180,66 +238,55 @@ struct Wave {
     }
     const float ks[2] = {a.scale_log2 * two_to(p.ek[0]), a.scale_log2 * two_to(p.ek[1])};
     float f[2] = {1.f, 1.f};
-    if (!kPBf16) {                             // f16: weights times 2^(ev - vref), at most 2^kSlack
-      const int top = max(p.ev[0], p.ev[1]);
-      if (top > vref) {
-        const float down = two_to(max(vref - top, -126));
-#pragma unroll
-        for (int g = 0; g < NQ; ++g)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[g][i] *= down;
-        vref = top;
-      }
-      f[0] = two_to(max(p.ev[0] - vref, -126));
-      f[1] = two_to(max(p.ev[1] - vref, -126));
-    }
+    if (!kPBf16) weigh(p.ev, f);
     uint4 w[NQ];
 #pragma unroll
-    for (int g = 0; g < NQ; ++g) {
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = s[g][i >> 2][i & 3] * ks[i >> 2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (p.tok[i] + kTile - 1 > u.pos0) {
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-            if (p.tok[i] + c * 4 + y > lim[g]) x[i * 4 + y] = -INFINITY;
-        }
-      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__any(mx > m[g] + kSlack)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-        // (a column that does not need it stays, so that no row's result depends on its neighbours)
-        const float to = mx > m[g] + kSlack ? mx : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
-        m[g] = to;
-        l[g] *= down;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[g][i] *= down;
-      }
-      float pr[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(x[i] - m[g]);
-      l[g] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-      u32 ww[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float p0 = pr[2 * i], p1 = pr[2 * i + 1];
-        if (!kPBf16) { p0 *= f[i >> 1]; p1 *= f[i >> 1]; }
-        ww[i] = pack2<kPBf16>(p0, p1);
-        if (DUP) {
-          const u32 rest = pack2<true>(p0 - as_f32(ww[i] << 16), p1 - as_f32(ww[i] & 0xffff0000u));
-          ww[i] = n & 8 ? rest : ww[i];
-        }
-      }
-      w[g] = make_uint4(ww[0], ww[1], ww[2], ww[3]);
-    }
+    for (int g = 0; g < NQ; ++g) w[g] = soften(g, s[g], p.tok, ks, f);
     const float v0 = kPBf16 ? two_to(p.ev[0]) : 1.f, v1 = kPBf16 ? two_to(p.ev[1]) : 1.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const auto v = widen<kPBf16>(word(p.v[0][i >> 2], i & 3), word(p.v[1][i >> 2], i & 3), v0, v1);
 #pragma unroll
       for (int g = 0; g < NQ; ++g) o[g][i] = mfma32<kPBf16>(v, __builtin_bit_cast(typename Op<kPBf16>::type, w[g]), o[g][i]);
+    }
+  }
+
+  // The same for pair x of a stage in LDS, already widened
+  template <class Lds>
+  __device__ __forceinline__ void take_staged(const Lds& lds, int stage, int x) {
+    int tok[2], ek[2], ev[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      tok[i] = __builtin_amdgcn_readfirstlane(lds.tok[stage][2 * x + i]);
+      ek[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ek[stage][2 * x + i]);
+      ev[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ev[stage][2 * x + i]);
+    }
+    f32x4 s[NQ][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) s[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const auto k = lds.k[stage][2 * x + i][j][lane];
+#pragma unroll
+        for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(k, q[g][j], s[g][i]);
+      }
+    }
+    float ks[2] = {a.scale_log2, a.scale_log2}, f[2] = {1.f, 1.f};
+    if (!BF16) {
+      ks[0] *= two_to(ek[0]);
+      ks[1] *= two_to(ek[1]);
+      weigh(ev, f);
+    }
+    uint4 w[NQ];
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) w[g] = soften(g, s[g], tok, ks, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const auto v = lds.v[stage][x][i][lane];
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) o[g][i] = mfma32<BF16>(v, __builtin_bit_cast(typename Op<BF16>::type, w[g]), o[g][i]);
     }
   }
 
@@ -262,6 +309,11 @@ struct Wave {
         take(p[1]);
       }
     }
+    close();
+  }
+
+  // Behind the last tile
+  __device__ __forceinline__ void close() {
     // a column's four lanes have a quarter of its sum each
 #pragma unroll
     for (int g = 0; g < NQ; ++g) {
@@ -444,10 +496,10 @@ __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL
 }
 
 // All tokens.  The units' tiles, one unit behind the other, are dealt out evenly: workgroup i has tiles [i, i + 1) * chunk of
-// them all, wherever units begin and end in there, so that lengths of any kind keep all CUs busy to the end.
-template <bool BF16, int NQ, bool DUP>
-__global__ __launch_bounds__(kAttnThreads, NQ == 4 ? 1 : 2) void q8_attn_dense_kernel(AttnArgs a) {
-  __shared__ AttnLds<NQ> lds;
+// them all, wherever units begin and end in there, so that lengths of any kind keep all CUs busy to the end.  A unit is up to
+// a.R rows of a sequence and a head; `each(u, t0, t1, tiles, f, count, mine, slot)` takes a piece of one.
+template <class Each>
+__device__ __forceinline__ void deal(const AttnArgs& a, Each each) {
   __shared__ u64 scan[kAttnWaves];
   __shared__ u64 s_base;
   __shared__ int s_seq;
@@ -498,9 +550,8 @@ __global__ __launch_bounds__(kAttnThreads, NQ == 4 ? 1 : 2) void q8_attn_dense_k
     s_seq = b;
   }
   __syncthreads();
-  Wave<BF16, NQ, DUP, false> w(a);
   u64 at = lo, base = s_base;
-  int b = __builtin_amdgcn_readfirstlane(s_seq), solo = 0;
+  int b = __builtin_amdgcn_readfirstlane(s_seq);
   while (at < hi && b < a.B) {
     int row0, rows, len, tiles;
     const int units = of(b, row0, rows, len, tiles) * a.H;
@@ -518,14 +569,120 @@ __global__ __launch_bounds__(kAttnThreads, NQ == 4 ? 1 : 2) void q8_attn_dense_k
       u.entries = min((len + a.P - 1) / a.P, a.NP);
       const int f = (int)(begin / chunk), count = (int)((begin + tiles - 1) / chunk) - f + 1;
       // a workgroup has the beginning of one unit that goes on behind it, and at most one piece that began before it
-      piece(a, w, lds, u, t0, t1, solo, count, (int)blockIdx.x * 2 + (t0 == 0 ? 1 : 0), f,
-            [&](int x) { return x == 0 ? f * 2 + 1 : (f + x) * 2; });
-      solo = (solo + 1) % kAttnWaves;
+      each(u, t0, t1, f, count, (int)blockIdx.x * 2 + (t0 == 0 ? 1 : 0), [f](int x) { return x == 0 ? f * 2 + 1 : (f + x) * 2; });
       at = begin + t1;
     }
     base = end;
     ++b;
   }
+}
+
+// A few rows of a sequence (up to 16 NQ columns): each wave has all of them and a part of the tokens.
+template <bool BF16, int NQ, bool DUP>
+__global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs a) {
+  __shared__ AttnLds<NQ> lds;
+  Wave<BF16, NQ, DUP, false> w(a);
+  int solo = 0;
+  deal(a, [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
+    piece(a, w, lds, u, t0, t1, solo, count, mine, f, slot);
+    solo = (solo + 1) % kAttnWaves;
+  });
+}
+
+// Many rows of a sequence: each wave has its own kRowGroups * 16 columns, and the workgroup goes through the tokens together,
+// 64 at a time: every wave fetches one tile, widens it and puts it into LDS in operand order, while the 64 before it are
+// taken; so a code is widened once for four waves.  Bound by the vector unit, which has an exponential for 4 x 128 products.
+constexpr int kRowGroups = 3;
+constexpr int kStageTiles = 4;
+template <bool BF16>
+struct RowsLds {
+  typedef typename Op<BF16>::type op;
+  op k[2][kStageTiles][4][kWave];              // [stage][tile][32 elements][lane]
+  op v[2][kStageTiles / 2][8][kWave];          // [stage][pair of tiles][16 elements][lane]
+  int tok[2][kStageTiles], ek[2][kStageTiles], ev[2][kStageTiles];
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs a) {
+  constexpr int NQ = kRowGroups;
+  __shared__ RowsLds<BF16> lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  Wave<BF16, NQ, false, false> w(a);
+  const int tpp = a.P / kTile, rows = a.R / kAttnWaves;                // of a page; of a wave
+  deal(a, [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
+    Unit u = whole;                            // this wave's rows
+    u.row0 += wave * rows;
+    u.pos0 += wave * rows;
+    u.rows = min(max(whole.rows - wave * rows, 0), rows);
+    const int last = u.pos0 + u.rows - 1;      // position of its last row
+    w.begin(u);
+    t1 = min(t1, max(t0, (whole.pos0 + whole.rows - 1) / kTile + 1));  // none of the rows sees more
+    uint4 raw[4];
+    int tok = kNowhere, ek = kExpMin, ev = kExpMin, e0 = -kWave, blk = -1, ex = 0;
+    auto fetch = [&](int t) {                  // tile t, this wave's of a stage
+      int b = -1;
+      ek = ev = kExpMin;
+      if (t < t1) {
+        const int e = t / tpp, sub = t - e * tpp;
+        if (e - e0 >= kWave) {                 // blocks and exponents of the next 64 pages
+          e0 = e;
+          const int i = e0 + w.lane;
+          blk = i < whole.entries ? a.table[(size_t)whole.seq * a.NP + i] : -1;
+          if ((unsigned)blk >= (unsigned)a.NB) blk = -1;
+          ex = blk >= 0 ? *reinterpret_cast<const int16_t*>(a.exps + ((size_t)blk * a.H + whole.h) * 2) : 0;
+        }
+        b = __builtin_amdgcn_readlane(blk, e - e0);
+        if (b >= 0) {
+          const int x = __builtin_amdgcn_readlane(ex, e - e0);
+          ek = (int8_t)x;
+          ev = (int8_t)(x >> 8);
+          const unsigned char* at = a.pages + (((size_t)b * a.H + whole.h) * tpp + sub) * kTileBytes + w.lane * 16;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const uint4*>(at + i * 1024);
+        }
+      }
+      tok = b >= 0 ? t * kTile : kNowhere;
+    };
+    auto put = [&](int s) {                    // into stage s; nothing where there is no tile: no column sees it, but it has to be finite
+      if (tok == kNowhere)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+      // (bf16 has the range to take the scales in; f16 has not, and theirs go into the logits and the weights)
+      const float sk = BF16 ? two_to(ek) : 1.f, sv = BF16 ? two_to(ev) : 1.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        lds.k[s][wave][j][w.lane] = widen<BF16>(word(raw[j >> 1], (j & 1) * 2), word(raw[j >> 1], (j & 1) * 2 + 1), sk, sk);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const uint4 x = __builtin_bit_cast(uint4, widen<BF16>(word(raw[2 + (i >> 2)], i & 3), word(raw[2 + (i >> 2)], (i & 3) + 1), sv, sv));
+        u64* to = reinterpret_cast<u64*>(&lds.v[s][wave >> 1][i][w.lane]) + (wave & 1);
+        to[0] = (u64)x.y << 32 | x.x;
+        to[2 * kWave] = (u64)x.w << 32 | x.z;  // (the next 16 elements' operand)
+      }
+      if (w.lane == 0) { lds.tok[s][wave] = tok; lds.ek[s][wave] = ek; lds.ev[s][wave] = ev; }
+    };
+    __syncthreads();                           // (the last piece's stages have been read)
+    if (t0 < t1) {
+      fetch(t0 + wave);
+      put(0);
+      __syncthreads();
+      int s = 0;
+      for (int t = t0; t < t1; t += kStageTiles, s ^= 1) {
+        const bool more = t + kStageTiles < t1;
+        if (more) fetch(t + kStageTiles + wave);
+        if (u.rows > 0 && t * kTile <= last) {
+#pragma unroll
+          for (int i = 0; i < kStageTiles / 2; ++i) w.take_staged(lds, s, i);
+        }
+        if (more) {
+          put(s ^ 1);
+          __syncthreads();
+        }
+      }
+    }
+    w.close();
+    finish_wave(a, w, count, mine * kAttnWaves + wave, f * kAttnWaves + wave, [&](int x) { return slot(x) * kAttnWaves + wave; });
+  });
 }
 
 // Selected pages: a unit is one row and head, in S pieces.
@@ -547,10 +704,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_selected_kernel(AttnA
         [&](int x) { return unit * a.S + x; });
 }
 
-// Columns of a unit's products in 16s: as many rows as a sequence has on the average, 64 columns at most
+// Columns of 16 that the rows of a sequence take, on the average: 1 and 2 go to waves that share the tokens, 0 (more) to
+// waves that share the columns
 static int column_groups(int T, int B, int G) {
-  const int want = (int)((T + B - 1) / B) * G;
-  return want <= 16 ? 1 : want <= 32 ? 2 : 4;
+  const int64_t want = (int64_t)((T + B - 1) / B) * G;
+  return want <= 16 ? 1 : want <= 32 ? 2 : 0;
+}
+// Columns of all partial results of a workgroup
+static int part_columns(int T, int B, int G) {
+  if (T <= B) return 8;
+  const int groups = column_groups(T, B, G);
+  return 16 * (groups ? groups : kAttnWaves * kRowGroups);
 }
 
 }  // namespace q8
@@ -558,8 +722,8 @@ static int column_groups(int T, int B, int G) {
 
 int64_t kvd_q8_attn_bytes(const kvd_q8_cache* c, const kvd_q8_rows* r) {
   using namespace kvd::q8;
-  const int cols = r->n_rows <= r->n_seqs ? 8 : 16 * column_groups(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
-  return (int64_t)kAttnGroups * 4 + (int64_t)2 * kAttnGroups * cols * kPartFloats * 4;
+  const int cols = part_columns(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
+  return (int64_t)kAttnGroups * kAttnWaves * 4 + (int64_t)2 * kAttnGroups * cols * kPartFloats * 4;
 }
 
 extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const void* q, int64_t q_stride, const int32_t* sel_pages,
@@ -580,7 +744,7 @@ extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const vo
   a.pages = static_cast<const unsigned char*>(c->pages); a.exps = c->exps;
   a.out = static_cast<uint16_t*>(out); a.lse = lse;
   a.ticket = static_cast<int32_t*>(workspace);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAttnGroups * 4);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAttnGroups * kAttnWaves * 4);
   a.B = r->n_seqs; a.NP = r->max_pages; a.T = r->n_rows; a.H = c->n_kv_heads; a.G = c->n_q_heads / c->n_kv_heads;
   a.P = c->page_size; a.NB = c->n_blocks; a.k = topk_pages;
   a.W = kAttnGroups;
@@ -607,15 +771,15 @@ extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const vo
     return launched();
   }
   const int groups = column_groups(a.T, a.B, a.G);
-  a.R = 16 * groups / a.G;
+  a.R = groups ? 16 * groups / a.G : 16 * kRowGroups / a.G * kAttnWaves;
   if (bf16) {
     if (groups == 1) go(q8_attn_dense_kernel<true, 1, false>);
     else if (groups == 2) go(q8_attn_dense_kernel<true, 2, false>);
-    else go(q8_attn_dense_kernel<true, 4, false>);
+    else go(q8_attn_rows_kernel<true>);
   } else {
     if (groups == 1) go(q8_attn_dense_kernel<false, 1, false>);
     else if (groups == 2) go(q8_attn_dense_kernel<false, 2, false>);
-    else go(q8_attn_dense_kernel<false, 4, false>);
+    else go(q8_attn_rows_kernel<false>);
   }
   return launched();
 }
