@@ -19,9 +19,12 @@ namespace q8 {
 
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnGroups = 512;               // workgroups of the dense form: two for each CU
+constexpr int kXcds = 8;                       // divides kAttnGroups
 constexpr int kLeastTiles = 16;                // tiles of a workgroup at least
 constexpr int kCoopTiles = 8;                  // from so many tiles on a piece is shared by the workgroup's waves
-constexpr int kPartFloats = kHeadDim + 4;      // a column's partial result: accumulators, maximum, sum
+constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
+// 8-byte words of a wave's partial result: accumulators, then a maximum and a sum a column
+__host__ __device__ constexpr size_t part_words(int groups) { return (size_t)groups * (16 * kWave + 16); }
 constexpr float kLowest = -3.0e38f, kSlack = 8.f;
 constexpr int kNowhere = 1 << 30;              // position of a tile that no row sees
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -33,7 +36,8 @@ struct AttnArgs {
   const unsigned char* pages;
   const int8_t* exps;
   uint16_t* out;
-  float *lse, *part;
+  float* lse;
+  u64* part;
   int32_t* ticket;
   int B, NP, T, H, G, P, NB, k, R, W, S;       // R rows of a unit, W workgroups (dense), S splits of a unit (selected)
   float scale_log2;
@@ -70,6 +74,9 @@ __device__ __forceinline__ typename Op<BF16>::type widen(u32 lo, u32 hi, float s
   return __builtin_bit_cast(typename Op<BF16>::type, make_uint4(w[0], w[1], w[2], w[3]));
 }
 __device__ __forceinline__ u32 word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+__device__ __forceinline__ u64 pack_floats(float a, float b) { return (u64)as_u32(b) << 32 | as_u32(a); }
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 // Two tiles on their way
 struct Pair {
@@ -180,47 +187,63 @@ struct Wave {
     f[1] = two_to(max(ev[1] - vref, -126));
   }
 
-  // The products q k of a column with the pair's tokens (four of each tile a lane) to weights, as the operand of the second
-  // product.  ks: what the products are taken times for logits in powers of two, f: the weights' factors (f16)
-  __device__ __forceinline__ uint4 soften(int g, const f32x4 (&s)[2], const int (&tok)[2], const float (&ks)[2], const float (&f)[2]) {
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3];
+  // The products q k of the columns with a pair's tokens (four of each tile a lane): hides what a column does not see, and
+  // raises the maxima where it has to.  ks: what the products are taken times for logits in powers of two
+  __device__ __forceinline__ void hide(f32x4 (&s)[NQ][2], const int (&tok)[2]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (tok[i] + kTile - 1 > u.pos0) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-          if (tok[i] + c * 4 + y > lim[g]) x[i * 4 + y] = -INFINITY;
+        for (int g = 0; g < NQ; ++g)
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (tok[i] + c * 4 + y > lim[g]) s[g][i][y] = -INFINITY;
       }
-    // (ks > 0 keeps the order)
-    float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * ks[0], fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])) * ks[1]);
-    if (__any(mx > m[g] + kSlack)) {
-      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-      // (a column that does not need it stays, so that no row's result depends on its neighbours)
-      const float to = mx > m[g] + kSlack ? mx : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
-      m[g] = to;
-      l[g] *= down;
+  }
+  __device__ __forceinline__ void raise(const f32x4 (&s)[NQ][2], const float (&ks)[2]) {
+    float mx[NQ];
+    bool any = false;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[g][i] *= down;
+    for (int g = 0; g < NQ; ++g) {             // (ks > 0 keeps the order)
+      mx[g] = fmaxf(fmaxf(max3(s[g][0][0], s[g][0][1], s[g][0][2]), s[g][0][3]) * ks[0],
+                    fmaxf(max3(s[g][1][0], s[g][1][1], s[g][1][2]), s[g][1][3]) * ks[1]);
+      any |= mx[g] > m[g] + kSlack;
     }
-    float pr[8];
+    if (__any(any)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], ks[i >> 2], -m[g]));
-    l[g] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-    u32 w[4];
+      for (int g = 0; g < NQ; ++g) {
+        mx[g] = fmaxf(mx[g], __shfl_xor(mx[g], 16, kWave));
+        mx[g] = fmaxf(mx[g], __shfl_xor(mx[g], 32, kWave));
+        // (a column that does not need it stays, so that no row's result depends on its neighbours)
+        const float to = mx[g] > m[g] + kSlack ? mx[g] : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
+        m[g] = to;
+        l[g] *= down;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float p0 = pr[2 * i], p1 = pr[2 * i + 1];
-      if (!kPBf16) { p0 *= f[i >> 1]; p1 *= f[i >> 1]; }
-      w[i] = pack2<kPBf16>(p0, p1);
-      if (DUP) {
-        const u32 rest = pack2<true>(p0 - as_f32(w[i] << 16), p1 - as_f32(w[i] & 0xffff0000u));
-        w[i] = n & 8 ? rest : w[i];
+        for (int i = 0; i < 8; ++i) o[g][i] *= down;
       }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  // The weights, as the operand of the second product.  f: their factors (f16)
+  __device__ __forceinline__ void soften(const f32x4 (&s)[NQ][2], const float (&ks)[2], const float (&f)[2], uint4 (&w)[NQ]) {
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+      float pr[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][i >> 2][i & 3], ks[i >> 2], -m[g]));
+      l[g] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+      u32 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float p0 = pr[2 * i], p1 = pr[2 * i + 1];
+        if (!kPBf16) { p0 *= f[i >> 1]; p1 *= f[i >> 1]; }
+        x[i] = pack2<kPBf16>(p0, p1);
+        if (DUP) {
+          const u32 rest = pack2<true>(p0 - as_f32(x[i] << 16), p1 - as_f32(x[i] & 0xffff0000u));
+          x[i] = n & 8 ? rest : x[i];
+        }
+      }
+      w[g] = make_uint4(x[0], x[1], x[2], x[3]);
+    }
   }
 
   __device__ __forceinline__ void take(const Pair& p) {
@@ -240,8 +263,9 @@ struct Wave {
     float f[2] = {1.f, 1.f};
     if (!kPBf16) weigh(p.ev, f);
     uint4 w[NQ];
-#pragma unroll
-    for (int g = 0; g < NQ; ++g) w[g] = soften(g, s[g], p.tok, ks, f);
+    hide(s, p.tok);
+    raise(s, ks);
+    soften(s, ks, f, w);
     const float v0 = kPBf16 ? two_to(p.ev[0]) : 1.f, v1 = kPBf16 ? two_to(p.ev[1]) : 1.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -251,42 +275,59 @@ struct Wave {
     }
   }
 
-  // The same for pair x of a stage in LDS, already widened
+  // The same for a stage of four tiles in LDS, already widened.  Operands are asked for four at a time, while the four before
+  // them are taken.
   template <class Lds>
-  __device__ __forceinline__ void take_staged(const Lds& lds, int stage, int x) {
-    int tok[2], ek[2], ev[2];
+  __device__ __forceinline__ void take_staged(const Lds& lds, int stage) {
+    typedef typename Op<BF16>::type op;
+    op b[2][4];
+    // keys of tile 0 and 1, values of pair 0 in two halves, then the same of pair 1
+    auto ask = [&](int i) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      tok[i] = __builtin_amdgcn_readfirstlane(lds.tok[stage][2 * x + i]);
-      ek[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ek[stage][2 * x + i]);
-      ev[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ev[stage][2 * x + i]);
-    }
-    f32x4 s[NQ][2];
+      for (int j = 0; j < 4; ++j)
+        b[i & 1][j] = i % 4 < 2 ? lds.k[stage][i / 4 * 2 + i % 4][j][lane] : lds.v[stage][i / 4][(i % 4 - 2) * 4 + j][lane];
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    ask(0);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int x = 0; x < 2; ++x) {
+      int tok[2], ek[2], ev[2];
 #pragma unroll
-      for (int g = 0; g < NQ; ++g) s[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const auto k = lds.k[stage][2 * x + i][j][lane];
-#pragma unroll
-        for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(k, q[g][j], s[g][i]);
+      for (int i = 0; i < 2; ++i) {
+        tok[i] = __builtin_amdgcn_readfirstlane(lds.tok[stage][2 * x + i]);
+        ek[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ek[stage][2 * x + i]);
+        ev[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ev[stage][2 * x + i]);
       }
-    }
-    float ks[2] = {a.scale_log2, a.scale_log2}, f[2] = {1.f, 1.f};
-    if (!BF16) {
-      ks[0] *= two_to(ek[0]);
-      ks[1] *= two_to(ek[1]);
-      weigh(ev, f);
-    }
-    uint4 w[NQ];
+      f32x4 s[NQ][2];
 #pragma unroll
-    for (int g = 0; g < NQ; ++g) w[g] = soften(g, s[g], tok, ks, f);
+      for (int i = 0; i < 2; ++i) {
+        ask(4 * x + i + 1);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const auto v = lds.v[stage][x][i][lane];
+        for (int g = 0; g < NQ; ++g) s[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int g = 0; g < NQ; ++g) o[g][i] = mfma32<BF16>(v, __builtin_bit_cast(typename Op<BF16>::type, w[g]), o[g][i]);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(b[i][j], q[g][j], s[g][i]);
+      }
+      float ks[2] = {a.scale_log2, a.scale_log2}, f[2] = {1.f, 1.f};
+      if (!BF16) {
+        ks[0] *= two_to(ek[0]);
+        ks[1] *= two_to(ek[1]);
+        weigh(ev, f);
+      }
+      hide(s, tok);
+      raise(s, ks);
+      uint4 w[NQ];
+      soften(s, ks, f, w);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (4 * x + i + 3 < 8) ask(4 * x + i + 3);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int g = 0; g < NQ; ++g)
+            o[g][i * 4 + j] = mfma32<BF16>(b[i][j], __builtin_bit_cast(op, w[g]), o[g][i * 4 + j]);
+      }
     }
   }
 
@@ -310,6 +351,57 @@ struct Wave {
       }
     }
     close();
+  }
+
+  // Partial results of other workgroups, as this launch's lanes have them: accumulators [g][i][half][lane] in pairs, then
+  // (maximum, sum) [g][n].  With DUP lanes n and n + 8 have the same.
+  __device__ __forceinline__ u64* part_of(int slot) const { return a.part + (size_t)slot * part_words(NQ); }
+  __device__ __forceinline__ void leave(int slot) const {
+    u64* part = part_of(slot);
+    if (DUP && (n & 8)) return;
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        store_agent(part + (g * 8 + i) * 2 * kWave + lane, pack_floats(o[g][i][0], o[g][i][1]));
+        store_agent(part + ((g * 8 + i) * 2 + 1) * kWave + lane, pack_floats(o[g][i][2], o[g][i][3]));
+      }
+      if (c == 0) store_agent(part + NQ * 16 * kWave + g * 16 + n, pack_floats(m[g], l[g]));
+    }
+  }
+  // The joined results slot(from), slot(from + step), ... of `count`
+  template <class Slot>
+  __device__ __forceinline__ void gather(int from, int step, int count, Slot slot) {
+    const int mine = DUP ? lane & ~8 : lane;
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+      m[g] = kLowest;
+      l[g] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int x = from; x < count; x += step) {
+      const u64* part = part_of(slot(x));
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) {
+        const u64 ml = load_agent(part + NQ * 16 * kWave + g * 16 + (mine & 15));
+        u64 v[8][2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v[i][0] = load_agent(part + (g * 8 + i) * 2 * kWave + mine);
+          v[i][1] = load_agent(part + ((g * 8 + i) * 2 + 1) * kWave + mine);
+        }
+        const float l2 = as_f32((u32)(ml >> 32)), m2 = l2 == 0.f ? kLowest : as_f32((u32)ml);
+        const float to = fmaxf(m[g], m2), f1 = __builtin_amdgcn_exp2f(m[g] - to), f2 = l2 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m2 - to);
+        m[g] = to;
+        l[g] = l[g] * f1 + l2 * f2;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const f32x4 y = {as_f32((u32)v[i][0]), as_f32((u32)(v[i][0] >> 32)), as_f32((u32)v[i][1]), as_f32((u32)(v[i][1] >> 32))};
+          o[g][i] = o[g][i] * f1 + y * f2;
+        }
+      }
+    }
   }
 
   // Behind the last tile
@@ -346,80 +438,49 @@ __device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, in
   if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Joins the `count` partial results of a unit; slot(i) is the i-th one's number.  By the threads tid, tid + nt, ...
-template <bool BF16, int COLS, bool DUP, class Slot>
-__device__ __forceinline__ void join(const AttnArgs& a, const Unit& u, int count, Slot slot, int tid, int nt) {
-  const int cols = DUP ? a.G : u.rows * a.G;
-  for (int x = tid; x < cols * 16; x += nt) {
-    const int col = x >> 4, d = (x & 15) * 8;
-    float M = kLowest;
-    for (int i = 0; i < count; ++i) {
-      const float* p = a.part + ((size_t)slot(i) * COLS + col) * kPartFloats + kHeadDim;
-      if (load_agent(p + 1) != 0.f) M = fmaxf(M, load_agent(p));
-    }
-    float L = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < count; ++i) {
-      const float* p = a.part + ((size_t)slot(i) * COLS + col) * kPartFloats;
-      const float l = load_agent(p + kHeadDim + 1);
-      if (l == 0.f) continue;                  // (nothing visible there, and no accumulators)
-      const float f = __builtin_amdgcn_exp2f(load_agent(p + kHeadDim) - M);
-      L += l * f;
-#pragma unroll
-      for (int y = 0; y < 8; ++y) v[y] += load_agent(p + d + y) * f;
-    }
-    emit<BF16>(a, u, col / a.G, col % a.G, d, v, M, L);
-  }
-}
-
 // Where a piece's result goes: to the output if it is all of the unit (count == 1), else to slot `mine` of the partial
-// results, which the last of the `count` pieces to arrive joins.
-template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
-__device__ __forceinline__ void finish_wave(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, int count, int mine, int ticket, Slot slot) {
-  constexpr int COLS = DUP ? 8 : 16 * NQ;
+// results, which the last of the `count` pieces to arrive joins, in their order; slot(i) is the i-th one's number.
+template <bool BF16, int NQ, bool DUP, bool SEL>
+__device__ __forceinline__ void emit_wave(const AttnArgs& a, const Wave<BF16, NQ, DUP, SEL>& w) {
 #pragma unroll
   for (int g = 0; g < NQ; ++g) {
     int r, head;
     w.column(g, r, head);
     if (!w.real(r, head) || (DUP && (w.n & 8))) continue;
-    if (count == 1) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v[4] = {w.o[g][i][0], w.o[g][i][1], w.o[g][i][2], w.o[g][i][3]};
-        emit<BF16>(a, w.u, r, head, i * 16 + w.c * 4, v, w.m[g], w.l[g]);
-      }
-    } else {
-      float* p = a.part + ((size_t)mine * COLS + r * a.G + head) * kPartFloats;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) store_agent(p + i * 16 + w.c * 4 + y, w.o[g][i][y]);
-      if (w.c == 0) { store_agent(p + kHeadDim, w.m[g]); store_agent(p + kHeadDim + 1, w.l[g]); }
+    for (int i = 0; i < 8; ++i) {
+      const float v[4] = {w.o[g][i][0], w.o[g][i][1], w.o[g][i][2], w.o[g][i][3]};
+      emit<BF16>(a, w.u, r, head, i * 16 + w.c * 4, v, w.m[g], w.l[g]);
     }
   }
-  if (count == 1) return;
-  wave_drain_memory();
-  int before = 0;
-  if (w.lane == 0) before = __hip_atomic_fetch_add(a.ticket + ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-  before = __builtin_amdgcn_readfirstlane(before);
-  if (before != count - 1) return;
-  if (w.lane == 0) store_agent(a.ticket + ticket, 0);
-  join<BF16, COLS, DUP>(a, w.u, count, slot, w.lane, kWave);
+}
+template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
+__device__ __forceinline__ void finish_wave(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, int count, int mine, int ticket, Slot slot) {
+  if (count > 1) {
+    w.leave(mine);                             // (written through and drained before the ticket, and read past the caches: no fence
+    wave_drain_memory();                       // of the ticket's, which would empty an XCD's L2: 583 us for 533 with it)
+    int before = 0;
+    if (w.lane == 0) before = __hip_atomic_fetch_add(a.ticket + ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    before = __builtin_amdgcn_readfirstlane(before);
+    if (before != count - 1) return;
+    if (w.lane == 0) store_agent(a.ticket + ticket, 0);
+    w.gather(0, 1, count, slot);
+  }
+  emit_wave(a, w);
 }
 
 template <int NQ>
 struct AttnLds {
   float ml[kAttnWaves][16 * NQ][2];
-  __align__(16) float o[kAttnWaves][16][kPartFloats];
+  __align__(16) float o[kAttnWaves][16][kColFloats];
   int last;
 };
 
-// The same for a piece that the waves of the workgroup shared
-template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
-__device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, int count, int mine,
-                                             int ticket, Slot slot) {
-  constexpr int COLS = DUP ? 8 : 16 * NQ;
+// The waves' results of one unit as one: with to_slot < 0 to the output, else there
+template <bool BF16, int NQ, bool DUP, bool SEL>
+__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, int to_slot) {
   const int tid = threadIdx.x, wave = tid / kWave;
-  __syncthreads();                             // (earlier pieces have been read)
+  __syncthreads();                             // (what was there has been read)
 #pragma unroll
   for (int g = 0; g < NQ; ++g)
     if (w.c == 0) {
@@ -456,24 +517,33 @@ __device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, D
 #pragma unroll
         for (int i = 0; i < kAttnWaves; ++i) v[y] += lds.o[i][n][d + y];
       }
-      if (count == 1) emit<BF16>(a, w.u, r, head, d, v, top, L);
+      if (to_slot < 0) emit<BF16>(a, w.u, r, head, d, v, top, L);
       else {
-        float* p = a.part + ((size_t)mine * COLS + r * a.G + head) * kPartFloats;
+        u64* part = w.part_of(to_slot);
+        const int at = (g * 8 + d / 16) * 2 * kWave + d % 16 / 4 * 16 + n;   // as lanes d % 16 / 4 * 16 + n and 16 more leave it
 #pragma unroll
-        for (int y = 0; y < 8; ++y) store_agent(p + d + y, v[y]);
-        if (d == 0) { store_agent(p + kHeadDim, top); store_agent(p + kHeadDim + 1, L); }
+        for (int y = 0; y < 4; ++y) store_agent(part + at + (y & 1) * kWave + (y >> 1) * 16, pack_floats(v[2 * y], v[2 * y + 1]));
+        if (d == 0) store_agent(part + NQ * 16 * kWave + col, pack_floats(top, L));
       }
     }
   }
+}
+// The same as finish_wave for a piece that the waves of the workgroup shared
+template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
+__device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, int count, int mine,
+                                             int ticket, Slot slot) {
+  merge_waves(a, w, lds, count == 1 ? -1 : mine);
   if (count == 1) return;
   wave_drain_memory();
   __syncthreads();
-  if (tid == 0) {
-    lds.last = __hip_atomic_fetch_add(a.ticket + ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == count - 1;
+  if (threadIdx.x == 0) {
+    lds.last = __hip_atomic_fetch_add(a.ticket + ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == count - 1;
     if (lds.last) store_agent(a.ticket + ticket, 0);
   }
   __syncthreads();
-  if (lds.last) join<BF16, COLS, DUP>(a, w.u, count, slot, tid, kAttnThreads);
+  if (!lds.last) return;
+  w.gather(threadIdx.x / kWave, kAttnWaves, count, slot);
+  merge_waves(a, w, lds, -1);
 }
 
 // Tiles [t0, t1) of a unit: by all waves, or, a short piece, by wave `solo` alone.
@@ -498,25 +568,32 @@ __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL
 // All tokens.  The units' tiles, one unit behind the other, are dealt out evenly: workgroup i has tiles [i, i + 1) * chunk of
 // them all, wherever units begin and end in there, so that lengths of any kind keep all CUs busy to the end.  A unit is up to
 // a.R rows of a sequence and a head; `each(u, t0, t1, tiles, f, count, mine, slot)` takes a piece of one.
-template <class Each>
-__device__ __forceinline__ void deal(const AttnArgs& a, Each each) {
-  __shared__ u64 scan[kAttnWaves];
+__device__ __forceinline__ u64 uniform(u64 x) {
+  return (u64)(u32)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (u32)__builtin_amdgcn_readfirstlane((int)x);
+}
+// The first unit of a sequence has `first` tiles and every next one `more` more, which is what their last rows see, rounded up.
+template <int NT, class Each>
+__device__ __forceinline__ void deal(const AttnArgs& a, bool grow, Each each) {
+  __shared__ u64 scan[NT / kWave];
   __shared__ u64 s_base;
   __shared__ int s_seq;
   const int tid = threadIdx.x, lane = tid % kWave, wv = tid / kWave;
-  auto of = [&](int b, int& row0, int& rows, int& len, int& tiles) {   // returns units a head
+  const int more = grow ? (a.R + kTile - 1) / kTile : 0;
+  auto of = [&](int b, int& row0, int& rows, int& len, int& first) {   // returns units a head
     row0 = min(max(a.row_start[b], 0), a.T);
     rows = min(max(a.row_start[b + 1], row0), a.T) - row0;
     len = min(max(a.kv_len[b], 0), a.NP * a.P);
-    tiles = max((len + kTile - 1) / kTile, 1);
+    first = max(((grow ? min(len, max(len - rows, 0) + a.R) : len) + kTile - 1) / kTile, 1);
     return (rows + a.R - 1) / a.R;
   };
-  const int per = (a.B + kAttnThreads - 1) / kAttnThreads, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  // tiles of a sequence's first n units of a head
+  auto upto_unit = [&](u64 n, int first) { return n * first + n * (n - 1) / 2 * more; };
+  const int per = (a.B + NT - 1) / NT, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
   u64 mine = 0;
   for (int b = b0; b < b1; ++b) {
-    int row0, rows, len, tiles;
-    const int units = of(b, row0, rows, len, tiles);
-    mine += (u64)units * a.H * tiles;
+    int row0, rows, len, first;
+    const u64 units = of(b, row0, rows, len, first);
+    mine += upto_unit(units, first) * a.H;
   }
   u64 upto = mine;
 #pragma unroll
@@ -528,21 +605,25 @@ __device__ __forceinline__ void deal(const AttnArgs& a, Each each) {
   __syncthreads();
   u64 all = 0;
 #pragma unroll
-  for (int i = 0; i < kAttnWaves; ++i) {
+  for (int i = 0; i < NT / kWave; ++i) {
     if (i < wv) upto += scan[i];
     all += scan[i];
   }
   u64 chunk = (all + a.W - 1) / a.W;
   if (chunk < (u64)kLeastTiles) chunk = kLeastTiles;
-  const u64 lo = blockIdx.x * chunk, hi = min(lo + chunk, all);
+  // neighbours in the order of the units share keys and values: they go to one XCD, whose workgroups are every eighth, and its L2
+  const int groups = (int)((all + chunk - 1) / chunk), each_xcd = (groups + kXcds - 1) / kXcds;
+  if ((int)blockIdx.x / kXcds >= each_xcd) return;
+  const int group = blockIdx.x % kXcds * each_xcd + blockIdx.x / kXcds;
+  const u64 lo = group * chunk, hi = min(lo + chunk, all);
   if (lo >= all) return;
   if (upto - mine <= lo && lo < upto) {
     u64 base = upto - mine;
     int b = b0;
     for (; b < b1; ++b) {
-      int row0, rows, len, tiles;
-      const int units = of(b, row0, rows, len, tiles);
-      const u64 n = (u64)units * a.H * tiles;
+      int row0, rows, len, first;
+      const u64 units = of(b, row0, rows, len, first);
+      const u64 n = upto_unit(units, first) * a.H;
       if (lo < base + n) break;
       base += n;
     }
@@ -550,26 +631,41 @@ __device__ __forceinline__ void deal(const AttnArgs& a, Each each) {
     s_seq = b;
   }
   __syncthreads();
-  u64 at = lo, base = s_base;
+  u64 at = uniform(lo), base = uniform(s_base);
+  const u64 per_group = uniform(chunk), stop = uniform(hi);
   int b = __builtin_amdgcn_readfirstlane(s_seq);
-  while (at < hi && b < a.B) {
-    int row0, rows, len, tiles;
-    const int units = of(b, row0, rows, len, tiles) * a.H;
-    const u64 end = base + (u64)units * tiles;
-    while (at < min(end, hi)) {
-      const u64 i = (at - base) / tiles, begin = base + i * tiles;
-      const int t0 = (int)(at - begin), t1 = (int)min((u64)tiles, hi - begin);
-      const int part = (int)(i / a.H);
+  while (at < stop && b < a.B) {
+    int row0, rows, len, first;
+    const int units = __builtin_amdgcn_readfirstlane(of(b, row0, rows, len, first));
+    row0 = __builtin_amdgcn_readfirstlane(row0);
+    rows = __builtin_amdgcn_readfirstlane(rows);
+    len = __builtin_amdgcn_readfirstlane(len);
+    first = __builtin_amdgcn_readfirstlane(first);
+    const u64 end = base + upto_unit(units, first) * a.H;
+    while (at < min(end, stop)) {
+      // unit `part` of its head: the largest one that begins at or before `at`, a head's units one behind the other
+      const u64 of_head = upto_unit(units, first), x = at - base, h = x / of_head, in = x - h * of_head;
+      u64 part;
+      if (more == 0) part = in / first;
+      else {                                   // first n + more n (n - 1) / 2 <= in, put right by whole numbers
+        const float p = first - 0.5f * more;
+        part = (u64)fmaxf((sqrtf(p * p + 2.f * more * (float)in) - p) / more, 0.f);
+        while (part > 0 && upto_unit(part, first) > in) --part;
+        while (upto_unit(part + 1, first) <= in) ++part;
+        part = uniform(part);
+      }
+      const u64 begin = base + h * of_head + upto_unit(part, first);
+      const int tiles = first + (int)part * more, t0 = (int)(at - begin), t1 = (int)min((u64)tiles, stop - begin);
       Unit u;
       u.seq = b;
-      u.h = (int)(i - (u64)part * a.H);
-      u.row0 = row0 + part * a.R;
-      u.rows = min(a.R, rows - part * a.R);
-      u.pos0 = len - rows + part * a.R;
+      u.h = (int)h;
+      u.row0 = row0 + (int)part * a.R;
+      u.rows = min(a.R, rows - (int)part * a.R);
+      u.pos0 = len - rows + (int)part * a.R;
       u.entries = min((len + a.P - 1) / a.P, a.NP);
-      const int f = (int)(begin / chunk), count = (int)((begin + tiles - 1) / chunk) - f + 1;
+      const int f = (int)(begin / per_group), count = (int)((begin + tiles - 1) / per_group) - f + 1;
       // a workgroup has the beginning of one unit that goes on behind it, and at most one piece that began before it
-      each(u, t0, t1, f, count, (int)blockIdx.x * 2 + (t0 == 0 ? 1 : 0), [f](int x) { return x == 0 ? f * 2 + 1 : (f + x) * 2; });
+      each(u, t0, t1, f, count, group * 2 + (t0 == 0 ? 1 : 0), [f](int x) { return x == 0 ? f * 2 + 1 : (f + x) * 2; });
       at = begin + t1;
     }
     base = end;
@@ -583,7 +679,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs
   __shared__ AttnLds<NQ> lds;
   Wave<BF16, NQ, DUP, false> w(a);
   int solo = 0;
-  deal(a, [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<kAttnThreads>(a, false, [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
     piece(a, w, lds, u, t0, t1, solo, count, mine, f, slot);
     solo = (solo + 1) % kAttnWaves;
   });
@@ -591,9 +687,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs
 
 // Many rows of a sequence: each wave has its own kRowGroups * 16 columns, and the workgroup goes through the tokens together,
 // 64 at a time: every wave fetches one tile, widens it and puts it into LDS in operand order, while the 64 before it are
-// taken; so a code is widened once for four waves.  Bound by the vector unit, which has an exponential for 4 x 128 products.
-constexpr int kRowGroups = 3;
-constexpr int kStageTiles = 4;
+// taken; so a code is widened once for four waves.  Bound by the matrix cores and the vector unit alike (an exponential takes
+// as long as 8 x 128 products).
+constexpr int kRowGroups = 2;
+constexpr int kStageTiles = kAttnWaves;
 template <bool BF16>
 struct RowsLds {
   typedef typename Op<BF16>::type op;
@@ -608,8 +705,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
   __shared__ RowsLds<BF16> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Wave<BF16, NQ, false, false> w(a);
-  const int tpp = a.P / kTile, rows = a.R / kAttnWaves;                // of a page; of a wave
-  deal(a, [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
+  const int tpp = a.P / kTile, rows = a.R / kAttnWaves;                // tiles of a page; rows of a wave
+  deal<kAttnThreads>(a, true, [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
     u.row0 += wave * rows;
     u.pos0 += wave * rows;
@@ -619,7 +716,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
     t1 = min(t1, max(t0, (whole.pos0 + whole.rows - 1) / kTile + 1));  // none of the rows sees more
     uint4 raw[4];
     int tok = kNowhere, ek = kExpMin, ev = kExpMin, e0 = -kWave, blk = -1, ex = 0;
-    auto fetch = [&](int t) {                  // tile t, this wave's of a stage
+    auto fetch = [&](int t) {                  // this wave's tile of the stage that begins with tile t
+      t += wave;
       int b = -1;
       ek = ev = kExpMin;
       if (t < t1) {
@@ -643,7 +741,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
       }
       tok = b >= 0 ? t * kTile : kNowhere;
     };
-    auto put = [&](int s) {                    // into stage s; nothing where there is no tile: no column sees it, but it has to be finite
+    auto put = [&](int s) {                    // zeros where there is no tile: no column sees it, but it has to be finite
       if (tok == kNowhere)
 #pragma unroll
         for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
@@ -663,17 +761,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
     };
     __syncthreads();                           // (the last piece's stages have been read)
     if (t0 < t1) {
-      fetch(t0 + wave);
+      fetch(t0);
       put(0);
       __syncthreads();
       int s = 0;
       for (int t = t0; t < t1; t += kStageTiles, s ^= 1) {
         const bool more = t + kStageTiles < t1;
-        if (more) fetch(t + kStageTiles + wave);
-        if (u.rows > 0 && t * kTile <= last) {
-#pragma unroll
-          for (int i = 0; i < kStageTiles / 2; ++i) w.take_staged(lds, s, i);
-        }
+        if (more) fetch(t + kStageTiles);
+        if (u.rows > 0 && t * kTile <= last) w.take_staged(lds, s);
         if (more) {
           put(s ^ 1);
           __syncthreads();
@@ -710,11 +805,10 @@ static int column_groups(int T, int B, int G) {
   const int64_t want = (int64_t)((T + B - 1) / B) * G;
   return want <= 16 ? 1 : want <= 32 ? 2 : 0;
 }
-// Columns of all partial results of a workgroup
-static int part_columns(int T, int B, int G) {
-  if (T <= B) return 8;
-  const int groups = column_groups(T, B, G);
-  return 16 * (groups ? groups : kAttnWaves * kRowGroups);
+// 8-byte words of a workgroup's partial results: two pieces, of each wave where the waves have columns of their own
+static int64_t part_words_of_group(int T, int B, int G) {
+  const int groups = T <= B ? 1 : column_groups(T, B, G);
+  return 2 * (int64_t)(groups ? part_words(groups) : kAttnWaves * part_words(kRowGroups));
 }
 
 }  // namespace q8
@@ -722,8 +816,7 @@ static int part_columns(int T, int B, int G) {
 
 int64_t kvd_q8_attn_bytes(const kvd_q8_cache* c, const kvd_q8_rows* r) {
   using namespace kvd::q8;
-  const int cols = part_columns(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
-  return (int64_t)kAttnGroups * kAttnWaves * 4 + (int64_t)2 * kAttnGroups * cols * kPartFloats * 4;
+  return (int64_t)kAttnGroups * kAttnWaves * 4 + kAttnGroups * 8 * part_words_of_group(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
 }
 
 extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const void* q, int64_t q_stride, const int32_t* sel_pages,
@@ -744,7 +837,7 @@ extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const vo
   a.pages = static_cast<const unsigned char*>(c->pages); a.exps = c->exps;
   a.out = static_cast<uint16_t*>(out); a.lse = lse;
   a.ticket = static_cast<int32_t*>(workspace);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kAttnGroups * kAttnWaves * 4);
+  a.part = reinterpret_cast<kvd::u64*>(static_cast<char*>(workspace) + kAttnGroups * kAttnWaves * 4);
   a.B = r->n_seqs; a.NP = r->max_pages; a.T = r->n_rows; a.H = c->n_kv_heads; a.G = c->n_q_heads / c->n_kv_heads;
   a.P = c->page_size; a.NB = c->n_blocks; a.k = topk_pages;
   a.W = kAttnGroups;
@@ -764,7 +857,7 @@ extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const vo
     return launched();
   }
   a.S = 1;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(kAttnGroups), dim3(kAttnThreads), 0, s, a); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.W), dim3(kAttnThreads), 0, s, a); };
   if (a.T <= a.B) {
     a.R = 1;
     if (bf16) go(q8_attn_dense_kernel<true, 1, true>); else go(q8_attn_dense_kernel<false, 1, true>);
