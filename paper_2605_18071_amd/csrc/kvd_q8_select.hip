@@ -1,7 +1,7 @@
 // Selection of pages by a score in 8 bits.  Two launches: the scores of all visible pages of every row and head, as
 // products of whole numbers on the matrix cores (int8, exact, so that the result does not depend on the order), and the k best
-// of a row and head by one workgroup, which holds the scores in registers and narrows the k-th one down by counting.
-// Scoring is bound by the memory (132 bytes a page and head), selecting by its trips to LDS.
+// of a row and head by one workgroup, which holds the scores in registers.  Scoring is bound by the memory (132 bytes a page and
+// head), selecting by its trips to LDS.
 #include "kvd_q8.h"
 
 namespace kvd {
@@ -32,7 +32,7 @@ __device__ __forceinline__ int pages_seen(const SelectArgs& a, int r, int& seq) 
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kScoreThreads) void q8_score_kernel(SelectArgs a) {
+__global__ __launch_bounds__(kScoreThreads, 4) void q8_score_kernel(SelectArgs a) {
   __shared__ __align__(16) int8_t qi[kScoreRows][kHeadDim];
   __shared__ int block_of[kScorePages];
   __shared__ int seen[kScoreRows];
@@ -58,8 +58,12 @@ __global__ __launch_bounds__(kScoreThreads) void q8_score_kernel(SelectArgs a) {
   for (int i = tid; i < np; i += kScoreThreads) block_of[i] = a.table[(size_t)seq * a.NP + p0 + i];
   // the queries in 8 bits: a wave a row, two elements a lane
   for (int i = w; i < kScoreRows; i += kScoreThreads / kWave) {
+    if (seen[i] == 0) {
+      *reinterpret_cast<uint16_t*>(&qi[i][lane * 2]) = 0;
+      continue;
+    }
     double s0 = 0.0, s1 = 0.0;
-    if (seen[i] > 0) {
+    {
       const uint16_t* q = a.q + (long long)(r0 + i) * a.q_stride + h * a.G * kHeadDim + lane * 2;
       for (int g = 0; g < a.G; ++g) {
         const u32 x = *reinterpret_cast<const u32*>(q + g * kHeadDim);
@@ -79,22 +83,37 @@ __global__ __launch_bounds__(kScoreThreads) void q8_score_kernel(SelectArgs a) {
   // 16 pages x 16 rows a product: lane l has page l % 16's (and row l % 16's) elements (l / 16) * 16 .. + 15 of each 64
   const int c = lane >> 4, n = lane & 15;
   const i32x4 q0 = *reinterpret_cast<const i32x4*>(&qi[n][c * 16]), q1 = *reinterpret_cast<const i32x4*>(&qi[n][64 + c * 16]);
-  for (int t = w * 16; t < np; t += kScoreThreads / kWave * 16) {
-    const int p = min(t + n, np - 1);
-    const int blk = block_of[p];
-    const bool good = (unsigned)blk < (unsigned)a.NB;
-    const size_t unit = (size_t)(good ? blk : 0) * a.H + h;
-    const i32x4* m = reinterpret_cast<const i32x4*>(a.means + unit * kHeadDim);
-    const i32x4 m0 = m[c], m1 = m[4 + c];
-    const float scale = good ? a.mean_scales[unit] : 0.f;
+  // (a wave has all its pages on their way before it takes the first)
+  constexpr int N = kScorePages / (kScoreThreads / kWave * 16);
+  i32x4 m0[N], m1[N];
+  float scale[N];
+  int good[N];
+#pragma unroll
+  for (int x = 0; x < N; ++x) {
+    const int t = (x * (kScoreThreads / kWave) + w) * 16;
+    good[x] = 0;
+    if (t < np) {
+      const int blk = block_of[min(t + n, np - 1)];
+      good[x] = (unsigned)blk < (unsigned)a.NB;
+      const size_t unit = (size_t)(good[x] ? blk : 0) * a.H + h;
+      const i32x4* m = reinterpret_cast<const i32x4*>(a.means + unit * kHeadDim);
+      m0[x] = m[c];
+      m1[x] = m[4 + c];
+      scale[x] = a.mean_scales[unit];
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < N; ++x) {
+    const int t = (x * (kScoreThreads / kWave) + w) * 16;
+    if (t >= np) continue;
     i32x4 dot = {0, 0, 0, 0};
-    dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q0, m0, dot, 0, 0, 0);   // rows of the result: query rows, columns: pages
-    dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q1, m1, dot, 0, 0, 0);
+    dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q0, m0[x], dot, 0, 0, 0);   // rows of the result: query rows, columns: pages
+    dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q1, m1[x], dot, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = c * 4 + i;
       if (t + n < np && p0 + t + n < seen[row])
-        a.scores[((size_t)(r0 + row) * a.H + h) * a.NP + p0 + t + n] = good ? (float)dot[i] * scale : -INFINITY;
+        a.scores[((size_t)(r0 + row) * a.H + h) * a.NP + p0 + t + n] = good[x] ? (float)dot[i] * scale[x] : -INFINITY;
     }
   }
 }
@@ -105,12 +124,19 @@ __device__ __forceinline__ u32 order_of(float s) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// KPT scores of a thread, neighbours
+// The k best of a row and head.  Scores are counted in bins of equal width between the least and the largest, which spreads them
+// (bins by their bits would not: most scores share a few exponents, and counting them would queue up at a few counters).  The bin
+// of the last page that is taken has a few pages then, which are compared with each other; should it have too many (scores that are
+// all alike, or have no finite range), their bits are gone through, 11 at a time.  KPT scores of a thread, neighbours.
+constexpr int kCandidates = 512;
 template <int KPT>
 __global__ __launch_bounds__(kSelectThreads) void q8_select_kernel(SelectArgs a) {
+  constexpr int NW = kSelectThreads / kWave;
   __shared__ u32 hist[kRadixBins];
-  __shared__ int scan[kSelectThreads / kWave + 1];
-  __shared__ int s_bin, s_below;
+  __shared__ int scan[NW + 1];
+  __shared__ float least[NW], largest[NW];
+  __shared__ u64 cand[kCandidates];
+  __shared__ int s_bin, s_below, s_cand;
   const int r = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
   int seq;
   const int n = pages_seen(a, r, seq);
@@ -123,56 +149,114 @@ __global__ __launch_bounds__(kSelectThreads) void q8_select_kernel(SelectArgs a)
     for (int i = tid; i < n; i += kSelectThreads) out[i] = i;
     return;
   }
+  // (n > k >= sink + recent: the forced pages are different ones)
   const float* s = a.scores + unit * a.NP;
-  u32 key[KPT];
+  float v[KPT];
+  float lo = INFINITY, hi = -INFINITY;
+  auto free_page = [&](int p) { return p < n && p >= a.sink && p < n - a.recent; };
 #pragma unroll
   for (int x = 0; x < KPT; ++x) {
     const int p = tid * KPT + x;
-    key[x] = 0;                                // behind the last: below every score
-    if (p < n) key[x] = p < a.sink || p >= n - a.recent ? 0xffffffffu : order_of(s[p]);
+    v[x] = p < n ? s[p] : 0.f;
+    if (free_page(p) && v[x] > -INFINITY) { lo = fminf(lo, v[x]); hi = fmaxf(hi, v[x]); }
   }
-  // the want-th largest key, from its highest bits down
-  u32 prefix = 0, mask = 0;
-  int need = want;
+  for (int i = tid; i < kRadixBins; i += kSelectThreads) hist[i] = 0;
+  lo = wave_allreduce_min(lo);
+  hi = wave_allreduce_max(hi);
+  if (tid % kWave == 0) { least[tid / kWave] = lo; largest[tid / kWave] = hi; }
+  if (tid == 0) s_cand = 0;
+  __syncthreads();
 #pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const u32 bits = pass == 2 ? 1023u : 2047u;
-    for (int i = tid; i < kRadixBins; i += kSelectThreads) hist[i] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < KPT; ++x)
-      if ((key[x] & mask) == prefix && tid * KPT + x < n) atomicAdd(&hist[(key[x] >> shift) & bits], 1u);
-    __syncthreads();
-    // bins from the top: thread t has bins 2047 - 2 t and the one below
-    const int hi = kRadixBins - 1 - 2 * tid;
-    const int c0 = (int)hist[hi], c1 = (int)hist[hi - 1];
+  for (int i = 0; i < NW; ++i) { lo = fminf(lo, least[i]); hi = fmaxf(hi, largest[i]); }
+  const float width = hi - lo;
+  const float per = width > 0.f && width < INFINITY ? (kRadixBins - 1) / width : 0.f;
+  // (every step of it keeps the order; NaN and what lies outside go to an end)
+  auto bin_of = [&](float x) { return (int)fminf(fmaxf((x - lo) * per, 0.f), (float)(kRadixBins - 1)); };
+  // the bin, of the counters, that has the need-th item from the top; how many lie above it
+  auto find = [&](int need) {
+    const int top = kRadixBins - 1 - 2 * tid;  // thread t has bins 2047 - 2 t and the one below
+    const int c0 = (int)hist[top], c1 = (int)hist[top - 1];
     int total;
     const int above = block_exclusive_scan<kSelectThreads>(c0 + c1, scan, total);
-    if (above < need && need <= above + c0) { s_bin = hi; s_below = above; }
-    else if (above + c0 < need && need <= above + c0 + c1) { s_bin = hi - 1; s_below = above + c0; }
+    if (above < need && need <= above + c0) { s_bin = top; s_below = above; }
+    else if (above + c0 < need && need <= above + c0 + c1) { s_bin = top - 1; s_below = above + c0; }
     __syncthreads();
-    prefix |= (u32)s_bin << shift;
-    mask |= bits << shift;
+  };
+#pragma unroll
+  for (int x = 0; x < KPT; ++x)
+    if (free_page(tid * KPT + x)) atomicAdd(&hist[bin_of(v[x])], 1u);
+  __syncthreads();
+  int need = want - min(a.sink, n) - min(a.recent, n);       // of the free pages
+  u32 in = 0, in_hi = 0;                       // bit x: page tid * KPT + x is taken
+  auto take = [&](int x) { if (x < 32) in |= 1u << x; else in_hi |= 1u << (x - 32); };
+  if (need > 0) {
+    find(need);
+    const int bin = s_bin, count = (int)hist[bin];
     need -= s_below;
-  }
-  // everything above the key, and the first `need` pages of the key itself, in page order
-  int above = 0, same = 0;
+    if (count <= kCandidates) {
 #pragma unroll
-  for (int x = 0; x < KPT; ++x)
-    if (tid * KPT + x < n) { above += key[x] > prefix; same += key[x] == prefix; }
-  int total;
-  const int same0 = block_exclusive_scan<kSelectThreads>(same, scan, total);
-  const int taken = min(max(need - same0, 0), same);
-  int at = block_exclusive_scan<kSelectThreads>(above + taken, scan, total);
-  int left = taken;
+      for (int x = 0; x < KPT; ++x) {
+        const int p = tid * KPT + x;
+        if (!free_page(p)) continue;
+        const int b = bin_of(v[x]);
+        if (b > bin) take(x);
+        if (b == bin) cand[atomicAdd(&s_cand, 1)] = (u64)order_of(v[x]) << 32 | (u32)~p;   // larger is better
+      }
+      __syncthreads();
 #pragma unroll
-  for (int x = 0; x < KPT; ++x)
-    if (tid * KPT + x < n) {
-      bool in = key[x] > prefix;
-      if (key[x] == prefix && left > 0) { in = true; --left; }
-      if (in) out[at++] = tid * KPT + x;
+      for (int x = 0; x < KPT; ++x) {
+        const int p = tid * KPT + x;
+        if (!free_page(p) || bin_of(v[x]) != bin) continue;
+        const u64 mine = (u64)order_of(v[x]) << 32 | (u32)~p;
+        int better = 0;
+        for (int i = 0; i < count; ++i) better += cand[i] > mine;
+        if (better < need) take(x);
+      }
+    } else {
+      u32 prefix = 0, mask = 0;
+#pragma unroll
+      for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const u32 bits = pass == 2 ? 1023u : 2047u;
+        __syncthreads();                       // (the counters have been read)
+        for (int i = tid; i < kRadixBins; i += kSelectThreads) hist[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < KPT; ++x)
+          if (free_page(tid * KPT + x) && bin_of(v[x]) == bin && (order_of(v[x]) & mask) == prefix)
+            atomicAdd(&hist[(order_of(v[x]) >> shift) & bits], 1u);
+        __syncthreads();
+        find(need);
+        prefix |= (u32)s_bin << shift;
+        mask |= bits << shift;
+        need -= s_below;
+      }
+      // of equal scores the lowest pages
+      int same = 0;
+#pragma unroll
+      for (int x = 0; x < KPT; ++x) same += free_page(tid * KPT + x) && bin_of(v[x]) == bin && order_of(v[x]) == prefix;
+      int total;
+      int left = need - block_exclusive_scan<kSelectThreads>(same, scan, total);
+#pragma unroll
+      for (int x = 0; x < KPT; ++x) {
+        if (!free_page(tid * KPT + x)) continue;
+        const int b = bin_of(v[x]);
+        const u32 key = order_of(v[x]);
+        if (b > bin || (b == bin && key > prefix)) take(x);
+        if (b == bin && key == prefix && left-- > 0) take(x);
+      }
     }
+  }
+#pragma unroll
+  for (int x = 0; x < KPT; ++x) {
+    const int p = tid * KPT + x;
+    if (p < n && !free_page(p)) take(x);
+  }
+  int total;
+  int at = block_exclusive_scan<kSelectThreads>(__popc(in) + __popc(in_hi), scan, total);
+#pragma unroll
+  for (int x = 0; x < KPT; ++x)
+    if ((x < 32 ? in >> x : in_hi >> (x - 32)) & 1) out[at++] = tid * KPT + x;
 }
 
 }  // namespace q8
@@ -210,6 +294,7 @@ extern "C" int kvd_q8_select(const kvd_q8_cache* c, const kvd_q8_rows* r, const 
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSelectThreads), 0, s, a); };
   if (a.NP <= 1024) go(q8_select_kernel<1>);
   else if (a.NP <= 4096) go(q8_select_kernel<4>);
+  else if (a.NP <= 8192) go(q8_select_kernel<8>);
   else if (a.NP <= 16384) go(q8_select_kernel<16>);
   else go(q8_select_kernel<64>);
   return launched();

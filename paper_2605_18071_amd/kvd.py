@@ -529,9 +529,9 @@ def _need(ok: bool, what: str):
 
 
 def _buffer(name: str, t: torch.Tensor, shape, dtype, device) -> torch.Tensor:
-    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.is_contiguous() and t.device == device,
-          f"{name}: a contiguous {dtype} tensor of {tuple(shape)} on {device} is wanted, "
-          f"got {t.dtype} of {tuple(t.shape)} on {t.device}")
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of {tuple(shape)} on {device} is wanted, "
+                         f"got {t.dtype} of {tuple(t.shape)} on {t.device}")
     return t
 
 
@@ -539,15 +539,17 @@ class _OnDevice:
     """Calls into the library with the tensors' GPU current, on `stream` or that GPU's current stream."""
 
     def _call(self, name: str, stream, *args):
-        index = self.device.index
-        _need(self.device.type == "cuda", f"{name}: tensors on a GPU are wanted, got {self.device}")
-        if stream is not None:
-            _need(stream.device == self.device, f"{name}: the stream is on {stream.device}, the tensors on {self.device}")
-        if torch.cuda.current_device() == index:
-            st = getattr(self.lib, name)(*args, _stream_handle(stream))
+        device = self.device
+        if device.type != "cuda":
+            raise ValueError(f"{name}: tensors on a GPU are wanted, got {device}")
+        if stream is not None and stream.device != device:
+            raise ValueError(f"{name}: the stream is on {stream.device}, the tensors on {device}")
+        handle = _stream_handle(stream or torch.cuda.current_stream(device.index))
+        if torch.cuda.current_device() == device.index:
+            st = getattr(self.lib, name)(*args, handle)
         else:
-            with torch.cuda.device(index):
-                st = getattr(self.lib, name)(*args, _stream_handle(stream))
+            with torch.cuda.device(device):
+                st = getattr(self.lib, name)(*args, handle)
         if st != OK:
             raise KvdError(st, name)
 
@@ -633,16 +635,18 @@ class Q8Cache(_OnDevice):
 
     def _rowed(self, name: str, t: torch.Tensor, heads: int, n_rows: int) -> int:
         """Stride of a [rows][heads][head_dim] tensor whose rows may lie apart."""
-        _need(t.shape == (n_rows, heads, self.head_dim) and t.dtype == self.kv_dtype and t.device == self.device
-              and t.stride(2) == 1 and t.stride(1) == self.head_dim,
-              f"{name}: a {self.kv_dtype} tensor of {(n_rows, heads, self.head_dim)} on {self.device} with whole rows is wanted, "
-              f"got {t.dtype} of {tuple(t.shape)}, strides {t.stride()} on {t.device}")
-        return t.stride(0) if n_rows > 1 else heads * self.head_dim
+        D = self.head_dim
+        row, head, element = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if t.shape != (n_rows, heads, D) or t.dtype is not self.kv_dtype or t.device != self.device or head != D or element != 1:
+            raise ValueError(f"{name}: a {self.kv_dtype} tensor of {(n_rows, heads, D)} on {self.device} with whole rows is wanted, "
+                             f"got {t.dtype} of {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+        return row if n_rows > 1 else heads * D
 
     def _check_rows(self, rows: Q8Rows, workspace: Optional[torch.Tensor] = None):
-        _need(rows.device == self.device, "the rows and the cache are on different devices")
-        if workspace is not None:
-            _need(workspace.device == self.device and workspace.is_contiguous(), "workspace: a contiguous tensor on the cache's device is wanted")
+        if rows.device != self.device:
+            raise ValueError("the rows and the cache are on different devices")
+        if workspace is not None and (workspace.device != self.device or not workspace.is_contiguous()):
+            raise ValueError("workspace: a contiguous tensor on the cache's device is wanted")
 
     def append(self, rows: Q8Rows, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
         """kvd_q8_append: the rows' keys and values [rows][kv heads][head_dim] into their pages."""
@@ -658,7 +662,7 @@ class Q8Cache(_OnDevice):
         k = sel_pages.shape[-1]
         _buffer("sel_pages", sel_pages, (rows.n_rows, self.n_kv_heads, k), torch.int32, self.device)
         self._call("kvd_q8_select", stream, self._ref, rows._ref, q.data_ptr(), qs, sel_pages.data_ptr(), k,
-                   workspace.data_ptr(), workspace.numel() * workspace.element_size())
+                   workspace.data_ptr(), workspace.nbytes)
 
     def attend(self, rows: Q8Rows, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, lse: Optional[torch.Tensor] = None,
                sel_pages: Optional[torch.Tensor] = None, stream=None):
@@ -673,4 +677,4 @@ class Q8Cache(_OnDevice):
             k = sel_pages.shape[-1]
             _buffer("sel_pages", sel_pages, (rows.n_rows, self.n_kv_heads, k), torch.int32, self.device)
         self._call("kvd_q8_attn", stream, self._ref, rows._ref, q.data_ptr(), qs, _ptr(sel_pages), k, out.data_ptr(), _ptr(lse),
-                   workspace.data_ptr(), workspace.numel() * workspace.element_size())
+                   workspace.data_ptr(), workspace.nbytes)
