@@ -21,7 +21,7 @@ constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnGroups = 512;               // workgroups of the dense form: two for each CU
 constexpr int kXcds = 8;                       // divides kAttnGroups
 constexpr int kLeastTiles = 16;                // tiles of a workgroup at least
-constexpr int kCoopTiles = 8;                  // from so many tiles on a piece is shared by the workgroup's waves
+constexpr int kCoopTiles = 8;                  // from so many tiles on a unit is shared by the workgroup's waves
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 // 8-byte words of a wave's partial result: accumulators, then a maximum and a sum a column
 __host__ __device__ constexpr size_t part_words(int groups) { return (size_t)groups * (16 * kWave + 16); }
@@ -546,17 +546,17 @@ __device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, D
   merge_waves(a, w, lds, -1);
 }
 
-// Tiles [t0, t1) of a unit: by all waves, or, a short piece, by wave `solo` alone.
+// Tiles [t0, t1) of a unit: by all waves, or, a short unit, by wave `solo` alone.
 template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
 __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, const Unit& u, int t0, int t1,
                                       int solo, int count, int mine, int ticket, Slot slot) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (!SEL) t1 = min(t1, max(t0, (u.pos0 + u.rows - 1) / kTile + 1));   // none of the rows sees more
-  if (t1 - t0 < kCoopTiles) {
+  if (count == 1 && t1 - t0 < kCoopTiles) {    // (pieces of one unit are joined in one way, whichever comes last: the sums' order is fixed)
     if (wave != solo) return;
     w.begin(u);
     w.sweep(t0, t1);
-    finish_wave(a, w, count, mine, ticket, slot);
+    emit_wave(a, w);
   } else {
     const int per = ((t1 - t0 + 1) / 2 + kAttnWaves - 1) / kAttnWaves * 2;
     w.begin(u);

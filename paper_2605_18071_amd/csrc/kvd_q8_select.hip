@@ -1,15 +1,18 @@
 // Selection of pages by a score in 8 bits.  Two launches: the scores of all visible pages of every row and head, as
-// products of whole numbers on the matrix cores (int8, exact, so that the result does not depend on the order), and the k best
+// products of whole numbers (int8, exact, so that the result does not depend on the order), and the k best
 // of a row and head by one workgroup, which holds the scores in registers.  Scoring is bound by the memory (132 bytes a page and
 // head), selecting by its trips to LDS.
+#include <type_traits>
+
 #include "kvd_q8.h"
 
 namespace kvd {
 namespace q8 {
 
 constexpr int kScoreThreads = 256;
-constexpr int kScorePages = 512;               // pages of a scoring workgroup
-constexpr int kScoreRows = 16;                 // rows of one sequence that share its reading of the index: columns of a product
+constexpr int kFewGroups = 512;                // workgroups below which a wave takes fewer pages: two for each CU
+constexpr int kScoreGroups = 768;              // workgroups from which on one takes several times that: three for each CU
+constexpr int kScoreRows = 16;                 // rows of one sequence that share its reading of the index
 constexpr int kSelectThreads = 1024;
 
 struct SelectArgs {
@@ -20,7 +23,7 @@ struct SelectArgs {
   const float* mean_scales;
   float* scores;                               // [T][H][NP]
   int32_t* sel;
-  int B, NP, T, H, G, P, NB, k, sink, recent;
+  int B, NP, T, H, G, P, NB, k, sink, recent, span;
 };
 
 // Pages that row r sees, 0 where it has no sequence or a position outside its table
@@ -31,90 +34,118 @@ __device__ __forceinline__ int pages_seen(const SelectArgs& a, int r, int& seq) 
   return pos / a.P + 1;
 }
 
-template <bool BF16>
+// One workgroup: 16 rows of a sequence and HG heads, PW pages a wave and step (64, and less where that would leave CUs without
+// work: 12 x 4 rows of 938 pages take 15 us with 64).  A load takes the entries of all these heads from one
+// page (8 lanes of 16 bytes a head): they are neighbours in memory, and a load whose lanes went to 16 pages, as operands of the
+// matrix cores would have it, waits for 16 address translations (45 us instead of 31 for 16 x 8192 pages of 8 heads).
+// The products are few enough for the vector unit: four elements an instruction.
+template <bool BF16, int HG, int PW>
 __global__ __launch_bounds__(kScoreThreads, 4) void q8_score_kernel(SelectArgs a) {
-  __shared__ __align__(16) int8_t qi[kScoreRows][kHeadDim];
-  __shared__ int block_of[kScorePages];
-  __shared__ int seen[kScoreRows];
-  const int r0 = blockIdx.x, h = blockIdx.y, p0 = blockIdx.z * kScorePages;
+  constexpr int kPages = 8 / HG;               // of a load
+  constexpr int kScorePages = kScoreThreads / kWave * PW;
+  __shared__ __align__(16) int8_t qi[HG][kScoreRows][kHeadDim];
   const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave;
-  // rows r0 .. r0 + n - 1: of one sequence, for the first of which this workgroup is
-  const int seq = a.row_seq[r0];
+  const int sub = lane / (8 * HG), x = lane / 8 % HG, k = lane % 8;          // page of the load, head, 16 elements
+  const int span = a.span * kScorePages;       // pages of this workgroup
+  const int r0 = blockIdx.x, h0 = blockIdx.y * HG, p0 = blockIdx.z * span;
+  const bool head = h0 + x < a.H;
+  // rows r0 .. r0 + 15, as far as they are of one sequence; lanes 16 apart have the same
+  const int n = lane & 15, r = min(r0 + n, a.T - 1), row_seq = a.row_seq[r], row_pos = a.row_pos[r];
+  const int seq = __builtin_amdgcn_readfirstlane(row_seq);
   if ((unsigned)seq >= (unsigned)a.B) return;
-  // (a row is the first of its sequence, or 16, 32, ... behind it: counted back, not taken from row_start, over rows of the same sequence)
-  const int back = r0 - a.row_start[seq];
-  if (back < 0 || back % kScoreRows != 0) return;
-  if (tid < kScoreRows) {
-    int s = -1, n = 0;
-    if (r0 + tid < a.T) n = pages_seen(a, r0 + tid, s);
-    seen[tid] = s == seq ? n : 0;
-  }
-  __syncthreads();
-  int most = 0;
+  const bool mine = row_seq == seq && r0 + n < a.T && row_pos >= 0 && row_pos < a.NP * a.P;
+  const int seen = mine ? row_pos / a.P + 1 : 0;
+  int most = seen;
 #pragma unroll
-  for (int i = 0; i < kScoreRows; ++i) most = max(most, seen[i]);
+  for (int y = 8; y >= 1; y >>= 1) most = max(most, __shfl_xor(most, y, kWave));
+  most = __builtin_amdgcn_readfirstlane(most);
   if (p0 >= most) return;
-  const int np = min(most - p0, kScorePages);
-  for (int i = tid; i < np; i += kScoreThreads) block_of[i] = a.table[(size_t)seq * a.NP + p0 + i];
-  // the queries in 8 bits: a wave a row, two elements a lane
-  for (int i = w; i < kScoreRows; i += kScoreThreads / kWave) {
-    if (seen[i] == 0) {
-      *reinterpret_cast<uint16_t*>(&qi[i][lane * 2]) = 0;
-      continue;
-    }
+  const int np = min(most - p0, span);
+  // (this workgroup is for rows 0, 16, 32, ... of a sequence)
+  const int back = r0 - a.row_start[seq];
+  const int32_t* table = a.table + (size_t)seq * a.NP + p0;
+  auto blocks_of = [&](int at) { return lane < PW && at + lane < np ? table[at + lane] : -1; };   // of the wave's pages from `at` on
+  int at = w * PW;
+  int blk = blocks_of(at);
+  if (back < 0 || back % kScoreRows != 0) return;
+  // the queries in 8 bits: a wave a row and head, two elements a lane
+  for (int i = w; i < kScoreRows * HG; i += kScoreThreads / kWave) {
+    const int row = i / HG, y = i % HG;
+    if (h0 + y >= a.H || __builtin_amdgcn_readlane(seen, row) == 0) continue;
+    const uint16_t* q = a.q + (long long)(r0 + row) * a.q_stride + (h0 + y) * a.G * kHeadDim + lane * 2;
+    u32 raw[KVD_MAX_GROUP];
+#pragma unroll
+    for (int g = 0; g < KVD_MAX_GROUP; ++g) raw[g] = g < a.G ? *reinterpret_cast<const u32*>(q + g * kHeadDim) : 0;
     double s0 = 0.0, s1 = 0.0;
-    {
-      const uint16_t* q = a.q + (long long)(r0 + i) * a.q_stride + h * a.G * kHeadDim + lane * 2;
-      for (int g = 0; g < a.G; ++g) {
-        const u32 x = *reinterpret_cast<const u32*>(q + g * kHeadDim);
-        if (BF16) { s0 += (double)as_f32(x << 16); s1 += (double)as_f32(x & 0xffff0000u); }
-        else { const f16x2 v = __builtin_bit_cast(f16x2, x); s0 += (double)(float)v.x; s1 += (double)(float)v.y; }
-      }
+#pragma unroll
+    for (int g = 0; g < KVD_MAX_GROUP; ++g) {
+      if (BF16) { s0 += (double)as_f32(raw[g] << 16); s1 += (double)as_f32(raw[g] & 0xffff0000u); }
+      else { const f16x2 v = __builtin_bit_cast(f16x2, raw[g]); s0 += (double)(float)v.x; s1 += (double)(float)v.y; }
     }
     double m = fmax(fabs(s0), fabs(s1));
 #pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) m = fmax(m, __shfl_xor(m, x, kWave));
+    for (int z = 32; z >= 1; z >>= 1) m = fmax(m, __shfl_xor(m, z, kWave));
     const double inv = 127.0 / m;
     const double a0 = s0 * inv, a1 = s1 * inv;
-    qi[i][lane * 2] = fabs(a0) < 128.0 ? (int8_t)rint(a0) : 0;       // (not for NaN)
-    qi[i][lane * 2 + 1] = fabs(a1) < 128.0 ? (int8_t)rint(a1) : 0;
+    const int i0 = fabs(a0) < 128.0 ? (int)rint(a0) : 0, i1 = fabs(a1) < 128.0 ? (int)rint(a1) : 0;     // (not for NaN)
+    *reinterpret_cast<uint16_t*>(&qi[y][row][lane * 2]) = (uint16_t)((i0 & 0xff) | (i1 & 0xff) << 8);
   }
   __syncthreads();
-  // 16 pages x 16 rows a product: lane l has page l % 16's (and row l % 16's) elements (l / 16) * 16 .. + 15 of each 64
-  const int c = lane >> 4, n = lane & 15;
-  const i32x4 q0 = *reinterpret_cast<const i32x4*>(&qi[n][c * 16]), q1 = *reinterpret_cast<const i32x4*>(&qi[n][64 + c * 16]);
-  // (a wave has all its pages on their way before it takes the first)
-  constexpr int N = kScorePages / (kScoreThreads / kWave * 16);
-  i32x4 m0[N], m1[N];
-  float scale[N];
-  int good[N];
+  // eight loads at a time
+  i32x4 m[2][8];
+  float scale[2][8];
+  auto ask = [&](int blocks, int first, i32x4 (&v)[8], float (&f)[8]) {        // pages first .. of those whose blocks these are
 #pragma unroll
-  for (int x = 0; x < N; ++x) {
-    const int t = (x * (kScoreThreads / kWave) + w) * 16;
-    good[x] = 0;
-    if (t < np) {
-      const int blk = block_of[min(t + n, np - 1)];
-      good[x] = (unsigned)blk < (unsigned)a.NB;
-      const size_t unit = (size_t)(good[x] ? blk : 0) * a.H + h;
-      const i32x4* m = reinterpret_cast<const i32x4*>(a.means + unit * kHeadDim);
-      m0[x] = m[c];
-      m1[x] = m[4 + c];
-      scale[x] = a.mean_scales[unit];
+    for (int i = 0; i < 8; ++i) {
+      const int b = __shfl(blocks, first + i * kPages + sub, kWave);
+      v[i] = i32x4{0, 0, 0, 0};
+      f[i] = -1.f;                             // a bad block
+      if (head && (unsigned)b < (unsigned)a.NB) {
+        const size_t unit = (size_t)b * a.H + h0 + x;
+        v[i] = *reinterpret_cast<const i32x4*>(a.means + unit * kHeadDim + k * 16);
+        f[i] = a.mean_scales[unit];
+      }
     }
-  }
+  };
+  auto take = [&](int first, const i32x4 (&v)[8], const float (&f)[8]) {
+    for (int row = 0; row < kScoreRows; ++row) {
+      const int sees = __builtin_amdgcn_readlane(seen, row);
+      if (sees == 0) continue;
+      const i32x4 q = *reinterpret_cast<const i32x4*>(&qi[x][row][k * 16]);
+      float score = 0.f;                       // of load k's page: every one of the eight lanes keeps one
 #pragma unroll
-  for (int x = 0; x < N; ++x) {
-    const int t = (x * (kScoreThreads / kWave) + w) * 16;
-    if (t >= np) continue;
-    i32x4 dot = {0, 0, 0, 0};
-    dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q0, m0[x], dot, 0, 0, 0);   // rows of the result: query rows, columns: pages
-    dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(q1, m1[x], dot, 0, 0, 0);
+      for (int i = 0; i < 8; ++i) {
+        int dot = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = c * 4 + i;
-      if (t + n < np && p0 + t + n < seen[row])
-        a.scores[((size_t)(r0 + row) * a.H + h) * a.NP + p0 + t + n] = good[x] ? (float)dot[i] * scale[x] : -INFINITY;
+        for (int y = 0; y < 4; ++y) dot = __builtin_amdgcn_sdot4(v[i][y], q[y], dot, false);
+        dot += __builtin_amdgcn_update_dpp(0, dot, 0xb1, 0xf, 0xf, true);    // quad_perm 1 0 3 2
+        dot += __builtin_amdgcn_update_dpp(0, dot, 0x4e, 0xf, 0xf, true);    // quad_perm 2 3 0 1
+        dot += __builtin_amdgcn_update_dpp(0, dot, 0x141, 0xf, 0xf, true);   // row_half_mirror: the other four of eight lanes
+        const float y = f[i] >= 0.f ? (float)dot * f[i] : -INFINITY;
+        if (k == i) score = y;
+      }
+      const int p = first + k * kPages + sub;
+      if (head && p < np && p0 + p < sees) a.scores[((size_t)(r0 + row) * a.H + h0 + x) * a.NP + p0 + p] = score;
     }
+  };
+  constexpr int kStep = 8 * kPages;            // pages of eight loads: 8 to 64
+  if (at < np) ask(blk, 0, m[0], scale[0]);
+  for (; at < np; at += kScorePages) {
+    const int next = blocks_of(at + kScorePages);
+#pragma unroll
+    for (int i = 0; i < PW; i += 2 * kStep) {  // (a step of all of them: what would be its second half is the next round's first)
+      if constexpr (kStep < PW) {
+        ask(blk, i + kStep, m[1], scale[1]);
+        take(at + i, m[0], scale[0]);
+        if (i + 2 * kStep < PW) ask(blk, i + 2 * kStep, m[0], scale[0]);
+        else ask(next, 0, m[0], scale[0]);
+        take(at + i + kStep, m[1], scale[1]);
+      } else {
+        take(at, m[0], scale[0]);
+        ask(next, 0, m[0], scale[0]);
+      }
+    }
+    blk = next;
   }
 }
 
@@ -285,9 +316,25 @@ extern "C" int kvd_q8_select(const kvd_q8_cache* c, const kvd_q8_rows* r, const 
   a.P = c->page_size; a.NB = c->n_blocks; a.k = topk_pages; a.sink = c->sink_pages; a.recent = c->recent_pages;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (a.NP > a.k) {                            // (otherwise no row has more pages than it takes)
-    const dim3 grid(a.T, a.H, (a.NP + kScorePages - 1) / kScorePages);
-    if (c->kv_dtype == KVD_BF16) hipLaunchKernelGGL(q8_score_kernel<true>, grid, dim3(kScoreThreads), 0, s, a);
-    else hipLaunchKernelGGL(q8_score_kernel<false>, grid, dim3(kScoreThreads), 0, s, a);
+    // (a grid's first dimension holds the rows, its third at most 1024 workgroups)
+    const int heads = a.H >= 5 ? 8 : a.H >= 3 ? 4 : a.H;
+    const int head_groups = (a.H + heads - 1) / heads;
+    auto steps = [&](int pages) { return (a.NP + pages - 1) / pages; };       // of a workgroup
+    const bool few = (int64_t)a.T * head_groups * steps(kScoreThreads) < kFewGroups;
+    const int pages = kScoreThreads / kWave * (few ? heads == 1 ? 64 : heads == 2 ? 32 : 16 : 64);
+    const int64_t most = (int64_t)a.T * head_groups * steps(pages);
+    a.span = few ? 1 : (int)(most / kScoreGroups < 16 ? most / kScoreGroups : 16);
+    const dim3 grid(a.T, head_groups, (steps(pages) + a.span - 1) / a.span);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kScoreThreads), 0, s, a); };
+    auto go_type = [&](auto type) {
+      constexpr bool BF16 = decltype(type)::value;
+      if (heads == 8) { if (few) go(q8_score_kernel<BF16, 8, 16>); else go(q8_score_kernel<BF16, 8, 64>); }
+      else if (heads == 4) { if (few) go(q8_score_kernel<BF16, 4, 16>); else go(q8_score_kernel<BF16, 4, 64>); }
+      else if (heads == 2) { if (few) go(q8_score_kernel<BF16, 2, 32>); else go(q8_score_kernel<BF16, 2, 64>); }
+      else go(q8_score_kernel<BF16, 1, 64>);
+    };
+    if (c->kv_dtype == KVD_BF16) go_type(std::true_type{});
+    else go_type(std::false_type{});
     if (int e = launched()) return e;
   }
   const dim3 grid(a.T, a.H);
