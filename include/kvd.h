@@ -549,8 +549,8 @@ int kvd_q8_append(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void
                   const void* v_new, int64_t v_stride, void* stream);
 
 /* Bytes of workspace that kvd_q8_attn (select == 0) or kvd_q8_select (select != 0) needs for these sizes; negative: a
- * kvd_status.  Zero it once; every call leaves it ready for the next.  A call that runs, or a graph that is replayed, at the
- * same time as another needs a workspace of its own. */
+ * kvd_status.  Zero it once; every call leaves it ready for the next, of either kind and of any sizes that it is large enough
+ * for.  A call that runs, or a graph that is replayed, at the same time as another needs a workspace of its own. */
 int64_t kvd_q8_workspace_bytes(const kvd_q8_cache* cache, const kvd_q8_rows* rows, int32_t select);
 
 /* Selects pages for every row and KV head by a score in 8 bits.

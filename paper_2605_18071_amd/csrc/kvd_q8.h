@@ -14,6 +14,9 @@ constexpr int kTile = 16;                      // tokens of a tile
 constexpr int kHalfTile = kTile * kHeadDim;    // bytes of a tile's keys, and of its values behind them
 constexpr int kTileBytes = 2 * kHalfTile;
 constexpr int kExpMin = -96;                   // least exponent of a scale: everything below 2^-105 is 0
+// What a workspace begins with: the attention's tickets, zero between calls.  The scores of a selection lie behind them, so that
+// one workspace may serve both calls, one after the other.
+constexpr int kTicketBytes = 8192;
 constexpr int kMaxSeqs = 4096, kMaxRows = 131072, kMaxHeads = 256, kMaxTablePages = 65536;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));

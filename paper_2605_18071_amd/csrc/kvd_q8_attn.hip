@@ -26,6 +26,7 @@ constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 // 8-byte words of a wave's partial result: accumulators, then a maximum and a sum a column
 __host__ __device__ constexpr size_t part_words(int groups) { return (size_t)groups * (16 * kWave + 16); }
 constexpr float kLowest = -3.0e38f, kSlack = 8.f;
+constexpr int kLift = 7;
 constexpr int kNowhere = 1 << 30;              // position of a tile that no row sees
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -91,7 +92,7 @@ struct Wave {
   float m[NQ], l[NQ];
   typename Op<BF16>::type q[NQ][4];
   int lim[NQ];                                 // last position that the lane's column sees
-  int vref;                                    // f16 values: accumulators hold 2^-vref of the result's numerator
+  int vref;                                    // f16 values: accumulators hold 2^(kLift - vref) of the result's numerator
 
   const AttnArgs& a;
   const int lane, c, n;
@@ -172,7 +173,8 @@ struct Wave {
     }
   }
 
-  // f16 values: weights are taken times 2^(ev - vref), at most 2^kSlack; vref follows the largest ev
+  // f16 values: weights are taken times 2^(ev - vref + kLift), at most 2^(kSlack + kLift), which f16 holds; vref follows the
+  // largest ev.  The lift keeps small weights, and those of pages with small values, among f16's normal numbers.
   __device__ __forceinline__ void weigh(const int (&ev)[2], float (&f)[2]) {
     const int top = max(ev[0], ev[1]);
     if (top > vref) {
@@ -183,8 +185,8 @@ struct Wave {
         for (int i = 0; i < 8; ++i) o[g][i] *= down;
       vref = top;
     }
-    f[0] = two_to(max(ev[0] - vref, -126));
-    f[1] = two_to(max(ev[1] - vref, -126));
+    f[0] = two_to(max(ev[0] - vref + kLift, -126));
+    f[1] = two_to(max(ev[1] - vref + kLift, -126));
   }
 
   // The products q k of the columns with a pair's tokens (four of each tile a lane): hides what a column does not see, and
@@ -412,7 +414,7 @@ struct Wave {
       l[g] += __shfl_xor(l[g], 16, kWave);
       l[g] += __shfl_xor(l[g], 32, kWave);
       if (!kPBf16) {
-        const float up = vref > -1000 ? two_to(vref) : 0.f;
+        const float up = vref > -1000 ? two_to(vref - kLift) : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[g][i] *= up;
       }
@@ -673,7 +675,9 @@ __device__ __forceinline__ void deal(const AttnArgs& a, bool grow, Each each) {
   }
 }
 
-// A few rows of a sequence (up to 16 NQ columns): each wave has all of them and a part of the tokens.
+// A few rows of a sequence (up to 16 NQ columns): each wave has all of them and a part of the tokens, with a pair of tiles on its
+// way behind the one it takes.  Bound by the memory: 16 x 32768 tokens of 8 heads 167 us (6.4 TB/s), 24 ragged contexts with up to
+// three rows of 7 x 4 heads 103 us (5.2 TB/s); short contexts by their chain of trips to memory (4 x 1000 tokens 14.5 us).
 template <bool BF16, int NQ, bool DUP>
 __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs a) {
   __shared__ AttnLds<NQ> lds;
@@ -687,8 +691,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs
 
 // Many rows of a sequence: each wave has its own kRowGroups * 16 columns, and the workgroup goes through the tokens together,
 // 64 at a time: every wave fetches one tile, widens it and puts it into LDS in operand order, while the 64 before it are
-// taken; so a code is widened once for four waves.  Bound by the matrix cores and the vector unit alike (an exponential takes
-// as long as 8 x 128 products).
+// taken; so a code is widened once for four waves.  Bound by the matrix cores and the vector unit alike, which two waves a SIMD hardly
+// get to work at the same time: 2 x 2048 rows of 32/8 heads behind 6144 tokens 533 us (900 TFLOP/s).  With 48 columns a wave
+// registers spill (818 us), with 64 and a SIMD's registers for one wave the vector unit's values land in accumulation registers
+// (800), with 32 a widened code serves fewer columns, but all fits.
 constexpr int kRowGroups = 2;
 constexpr int kStageTiles = kAttnWaves;
 template <bool BF16>
@@ -780,14 +786,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
   });
 }
 
-// Selected pages: a unit is one row and head, in S pieces.
+// Selected pages: a unit is one row and head, in S pieces, so that there are two workgroups for each CU.  16 x 8 units of 256 pages
+// 30 us (4.5 TB/s): the memory behind a chain of selection, table, exponents and pages.
 template <bool BF16>
 __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_selected_kernel(AttnArgs a) {
   __shared__ AttnLds<1> lds;
-  const int unit = blockIdx.x / a.S, s = blockIdx.x - unit * a.S;
   Unit u;
-  u.row0 = unit / a.H;
-  u.h = unit - u.row0 * a.H;
+  u.row0 = blockIdx.x;
+  u.h = blockIdx.y / a.S;
+  const int s = blockIdx.y - u.h * a.S, unit = u.row0 * a.H + u.h;
   u.rows = 1;
   u.seq = a.row_seq[u.row0];
   u.pos0 = a.row_pos[u.row0];
@@ -795,7 +802,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_selected_kernel(AttnA
   u.entries = min(a.k, u.pos0 / a.P + 1);
   const int tiles = u.entries * (a.P / kTile), per = (tiles + a.S - 1) / a.S;
   Wave<BF16, 1, true, true> w(a);
-  piece(a, w, lds, u, min(s * per, tiles), min((s + 1) * per, tiles), 0, a.S, (int)blockIdx.x, unit,
+  piece(a, w, lds, u, min(s * per, tiles), min((s + 1) * per, tiles), 0, a.S, unit * a.S + s, unit,
         [&](int x) { return unit * a.S + x; });
 }
 
@@ -816,7 +823,8 @@ static int64_t part_words_of_group(int T, int B, int G) {
 
 int64_t kvd_q8_attn_bytes(const kvd_q8_cache* c, const kvd_q8_rows* r) {
   using namespace kvd::q8;
-  return (int64_t)kAttnGroups * kAttnWaves * 4 + kAttnGroups * 8 * part_words_of_group(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
+  static_assert(kAttnGroups * kAttnWaves * 4 <= kTicketBytes, "a ticket for each wave of each workgroup");
+  return kTicketBytes + (int64_t)kAttnGroups * 8 * part_words_of_group(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
 }
 
 extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const void* q, int64_t q_stride, const int32_t* sel_pages,
@@ -837,7 +845,7 @@ extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const vo
   a.pages = static_cast<const unsigned char*>(c->pages); a.exps = c->exps;
   a.out = static_cast<uint16_t*>(out); a.lse = lse;
   a.ticket = static_cast<int32_t*>(workspace);
-  a.part = reinterpret_cast<kvd::u64*>(static_cast<char*>(workspace) + kAttnGroups * kAttnWaves * 4);
+  a.part = reinterpret_cast<kvd::u64*>(static_cast<char*>(workspace) + kTicketBytes);
   a.B = r->n_seqs; a.NP = r->max_pages; a.T = r->n_rows; a.H = c->n_kv_heads; a.G = c->n_q_heads / c->n_kv_heads;
   a.P = c->page_size; a.NB = c->n_blocks; a.k = topk_pages;
   a.W = kAttnGroups;
@@ -851,7 +859,7 @@ extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const vo
     if (S > tiles / kLeastTiles) S = tiles / kLeastTiles;
     a.S = S < 1 ? 1 : S;
     a.R = 1;
-    const dim3 grid((unsigned)(units * a.S));
+    const dim3 grid(a.T, a.H * a.S);
     if (bf16) hipLaunchKernelGGL(q8_attn_selected_kernel<true>, grid, dim3(kAttnThreads), 0, s, a);
     else hipLaunchKernelGGL(q8_attn_selected_kernel<false>, grid, dim3(kAttnThreads), 0, s, a);
     return launched();

@@ -329,7 +329,7 @@ def test_calls_on_two_streams_with_a_workspace_each():
     for (o, l), (wo, wl) in got:
         assert torch.equal(o, wo) and torch.equal(l, wl)
     # every call leaves the workspace ready: the counters at its start are zero again
-    assert int(wsa[:512].abs().max()) == 0 and int(wsb[:512].abs().max()) == 0
+    assert int(wsa[:2048].abs().max()) == 0 and int(wsb[:2048].abs().max()) == 0
 
 
 class Server:
@@ -435,3 +435,21 @@ def test_results_do_not_change_from_call_to_call():
     for _ in range(20):
         o, l = s.attend(q)
         assert torch.equal(o, first[0]) and torch.equal(l, first[1])
+
+
+def test_one_workspace_for_selections_and_attention_of_different_sizes():
+    """A workspace that is large enough for all of them serves one call after another, whatever ran in it before."""
+    steps = [Step([9000, 40], [1, 1], seed=21), Step([600, 700], [40, 9], dtype="f16", seed=22), Step([5000], [3], P=32, G=8, seed=23)]
+    need = max(t.numel() for s in steps for t in (s.cache.workspace(s.rows), s.cache.workspace(s.rows, select=True)))
+    ws = torch.zeros(need, dtype=torch.int32, device=DEV)
+    qs = [s.query() for s in steps]
+    alone = [(s.attend(q), _select(s, q, 9, 1, 1, rows=[])) for s, q in zip(steps, qs)]
+    for _ in range(3):
+        for s, q, (want, sel) in zip(steps, qs, alone):
+            got = torch.full_like(sel, -9)
+            s.cache.select(s.rows, q, got, ws)
+            out, lse = s.attend(q, ws=ws)
+            assert torch.equal(got, sel) and torch.equal(out, want[0]) and torch.equal(lse, want[1])
+            o2, l2 = s.attend(q, sel=got, ws=ws)
+            s.check_attention(q, o2, l2, got, rows=[0, s.real - 1])
+    assert int(ws[:2048].abs().max()) == 0
