@@ -569,7 +569,8 @@ __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL
 
 // All tokens.  The units' tiles, one unit behind the other, are dealt out evenly: workgroup i has tiles [i, i + 1) * chunk of
 // them all, wherever units begin and end in there, so that lengths of any kind keep all CUs busy to the end.  A unit is up to
-// a.R rows of a sequence and a head; `each(u, t0, t1, tiles, f, count, mine, slot)` takes a piece of one.
+// a.R rows of a sequence and a head; `each(u, t0, t1, f, count, mine, slot)` takes tiles [t0, t1) of one:
+// one of `count` pieces, whose partial result goes to slot `mine`; f numbers the unit's ticket.
 __device__ __forceinline__ u64 uniform(u64 x) {
   return (u64)(u32)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (u32)__builtin_amdgcn_readfirstlane((int)x);
 }
@@ -835,6 +836,7 @@ extern "C" int kvd_q8_attn(const kvd_q8_cache* c, const kvd_q8_rows* r, const vo
   if (!stride_ok(q_stride, c->n_q_heads)) return KVD_ERR_SHAPE;
   if (sel_pages != nullptr && (topk_pages < 1 || topk_pages > KVD_MAX_TOPK)) return KVD_ERR_SHAPE;
   if (!aligned(c->pages, 16) || !aligned(c->exps, 2) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return KVD_ERR_ARG;
+  if (out == q) return KVD_ERR_ARG;            // (a row's pieces read q while the first unit that is done writes)
   if ((reinterpret_cast<uintptr_t>(lse) & 3) || (reinterpret_cast<uintptr_t>(sel_pages) & 3)) return KVD_ERR_ARG;
   if (!aligned(r->page_table, 4) || !aligned(r->kv_len, 4) || !aligned(r->row_start, 4) || !aligned(r->row_seq, 4) || !aligned(r->row_pos, 4)) return KVD_ERR_ARG;
   if (workspace_bytes < kvd_q8_attn_bytes(c, r)) return KVD_ERR_CAPACITY;

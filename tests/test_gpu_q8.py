@@ -164,6 +164,14 @@ def test_select_among_many_pages(pages, k):
     _select(s, s.query(), k)
 
 
+@pytest.mark.parametrize("H", [1, 2, 3, 4, 5, 8, 9])
+@pytest.mark.parametrize("lens,news,max_pages", [([900, 2100], [1, 3], None), ([500, 3, 333] * 20, [10] * 60, None),
+                                                 ([2900, 700] * 10, [40, 1] * 10, 800)])
+def test_select_of_any_number_of_heads_for_few_rows_and_many(H, lens, news, max_pages):
+    s = Step(lens, news, P=16, H=H, G=2, seed=H, max_pages=max_pages)
+    _select(s, s.query(), 9, 1, 1, rows=range(0, s.real, 1 + s.real // 12))
+
+
 def test_select_with_equal_scores_bad_blocks_and_queries_that_are_no_numbers():
     s = Step([800, 800, 800], [1, 1, 1], seed=9)
     q = s.query()
@@ -210,6 +218,15 @@ def test_attend_long_and_ragged(dtype):
     s.check_attention(q, *s.attend(q))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("Gq", [2, 3, 5, 6])
+@pytest.mark.parametrize("lens,news", [([0, 37, 5], [290, 41, 1]), ([9000], [70])])
+def test_attend_many_rows_of_any_group(dtype, Gq, lens, news):
+    s = Step(lens, news, P=32, H=2, G=Gq, dtype=dtype, seed=Gq, spare=1)
+    q = s.query(2.0)
+    s.check_attention(q, *s.attend(q), rows=sorted(set(list(range(0, s.real, 23)) + [s.real - 2, s.real - 1])))
+
+
 def test_attend_many_short_sequences():
     rng = np.random.default_rng(5)
     lens = rng.integers(0, 60, 700).tolist()
@@ -219,6 +236,25 @@ def test_attend_many_short_sequences():
     s = Step(lens[:300], [2] * 300, H=2, G=2, seed=5)
     q = s.query()
     s.check_attention(q, *s.attend(q), rows=range(0, 600, 11))
+
+
+def test_attend_keeps_pages_of_small_values_beside_a_page_of_large_ones():
+    """f16: one page's values are 2^14 times as large as the others', and lies behind what most rows see."""
+    for news in ([1], [30], [60]):
+        s = Step([1000], news, dtype="f16", H=1, seed=31)
+        s.cache.exps[:, :, 1] = -9
+        s.cache.exps[int(s.table[0, (999 + news[0]) // 16]), :, 1] = 5
+        q = s.query(0.5)
+        out, lse = s.attend(q)
+        s.check_attention(q, out, lse)
+        # rows in front of that page: each of up to 1060 weights is off by 2^-11, or, below 2^-14 of 2^-7, by 2^-25 of it, and the output by 2^-11
+        ref = G.to_ref(s.cache, 16)
+        first = s.pos.index(next(p for p in s.pos if p // 16 == (999 + news[0]) // 16))
+        for r in range(0, first, 5):
+            o, _ = R.attend_row(ref, s.table[0], q[r].double().cpu().numpy(), 0, s.pos[r], 1 / np.sqrt(128.0))
+            big = np.abs(R.VALUES[ref.codes[s.table[0, : s.pos[r] // 16 + 1], 0, 1]]).max() * 2.0 ** -9
+            got = out[r].double().cpu().numpy()
+            assert np.abs(got - o).max() <= 2.0 ** -11 * np.abs(o).max() + (2.0 ** -11 + 2.0 ** -15) * big + 2.0 ** -25
 
 
 @pytest.mark.parametrize("news", [[1, 1], [9, 30]])

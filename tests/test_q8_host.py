@@ -93,10 +93,11 @@ def test_pointers_strides_and_workspaces():
 
     need = lib.kvd_q8_workspace_bytes(bc, br, 0)
 
-    def attn(cache=bc, rows=br, q=P, qs=1024, sel=None, k=0, out=P, lse=None, ws=P, n=need):
+    def attn(cache=bc, rows=br, q=P, qs=1024, sel=None, k=0, out=8 * P, lse=None, ws=P, n=need):
         return lib.kvd_q8_attn(cache, rows, q, qs, sel, k, out, lse, ws, n, None)
 
     assert attn(cache=None) == attn(rows=None) == attn(q=None) == attn(out=None) == attn(ws=None) == kvd.ERR_ARG
+    assert attn(out=P) == kvd.ERR_ARG                     # in place: pieces of a row still read what others write
     assert attn(out=P + 8) == attn(lse=P + 1) == attn(sel=P + 2, k=4) == attn(rows=C.byref(_rows(kv_len=None))) == kvd.ERR_ARG
     assert attn(qs=0) == attn(sel=P, k=0) == attn(sel=P, k=2049) == kvd.ERR_SHAPE
     assert attn(n=need - 1) == kvd.ERR_CAPACITY
