@@ -161,8 +161,8 @@ struct Wave {
         const unsigned char* at = a.pages + (((size_t)b * a.H + u.h) * tpp + sub) * kTileBytes + lane * 16;
         p.k[i][0] = load_stream16(at);
         p.k[i][1] = load_stream16(at + 1024);
-        p.v[i][0] = load_stream16(at + 2048);
-        p.v[i][1] = load_stream16(at + 3072);
+        p.v[i][0] = load_stream16(at + kHalfTile);
+        p.v[i][1] = load_stream16(at + kHalfTile + 1024);
       } else {
         p.tok[i] = kNowhere;
         p.ek[i] = p.ev[i] = kExpMin;
