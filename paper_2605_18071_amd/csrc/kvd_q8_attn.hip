@@ -9,9 +9,13 @@
 // more than kSlack, so that the accumulators are rarely touched; p then stays below 2^kSlack, and nothing is lost, as all of this
 // is floating point.
 //
-// DUP (one row of up to 8 heads): the 16 columns hold each head twice, and the second copy takes what rounding P to
-// bf16 left of it: P is then 16 bits long at the price of nothing, as the columns would be empty.  Otherwise P is rounded to
-// the type of q, half a step of 2^-9 (bf16) or 2^-12 (f16) of each weight, like the output.
+// Weights and values go to the second product in bf16, which has the range for any scale of a page: no page's scale, seen or
+// hidden, costs another page's tokens anything.  (f16 has not: weights relative to the largest scale of a wave's pages lost
+// all their bits where values were 2^30 apart.)  The weights' bits: DUP (one row of up to 8 heads): the 16 columns hold each head
+// twice, and the second copy takes what rounding P to bf16 left of it: P is then 16 bits long at the price of nothing, as the
+// columns would be empty.  TWO: a product more for that rest, which costs 2 % where a few rows wait for the memory.  Many rows of bf16
+// do without it: P is rounded to bf16 there, by 2^-8 of each weight at most, like their output (530 us for 670 with it at 2 x 2048 rows of 32/8
+// heads behind 6144 tokens; f16, whose outputs show it, 698).
 #include "kvd_q8.h"
 
 namespace kvd {
@@ -26,7 +30,6 @@ constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 // 8-byte words of a wave's partial result: accumulators, then a maximum and a sum a column
 __host__ __device__ constexpr size_t part_words(int groups) { return (size_t)groups * (16 * kWave + 16); }
 constexpr float kLowest = -3.0e38f, kSlack = 8.f;
-constexpr int kLift = 7;
 constexpr int kNowhere = 1 << 30;              // position of a tile that no row sees
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -85,14 +88,13 @@ struct Pair {
   int tok[2], ek[2], ev[2];
 };
 
-template <bool BF16, int NQ, bool DUP, bool SEL>
+template <bool BF16, int NQ, bool DUP, bool TWO, bool SEL>
 struct Wave {
-  static constexpr bool kPBf16 = DUP || BF16;  // P and V in bf16
+  static constexpr int kParts = TWO ? 2 : 1;   // operands of P
   f32x4 o[NQ][8];
   float m[NQ], l[NQ];
   typename Op<BF16>::type q[NQ][4];
   int lim[NQ];                                 // last position that the lane's column sees
-  int vref;                                    // f16 values: accumulators hold 2^(kLift - vref) of the result's numerator
 
   const AttnArgs& a;
   const int lane, c, n;
@@ -111,7 +113,6 @@ struct Wave {
 
   __device__ __forceinline__ void begin(const Unit& unit) {
     u = unit;
-    vref = -1000;
 #pragma unroll
     for (int g = 0; g < NQ; ++g) {
       int r, head;
@@ -173,22 +174,6 @@ struct Wave {
     }
   }
 
-  // f16 values: weights are taken times 2^(ev - vref + kLift), at most 2^(kSlack + kLift), which f16 holds; vref follows the
-  // largest ev.  The lift keeps small weights, and those of pages with small values, among f16's normal numbers.
-  __device__ __forceinline__ void weigh(const int (&ev)[2], float (&f)[2]) {
-    const int top = max(ev[0], ev[1]);
-    if (top > vref) {
-      const float down = two_to(max(vref - top, -126));
-#pragma unroll
-      for (int g = 0; g < NQ; ++g)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[g][i] *= down;
-      vref = top;
-    }
-    f[0] = two_to(max(ev[0] - vref + kLift, -126));
-    f[1] = two_to(max(ev[1] - vref + kLift, -126));
-  }
-
   // The products q k of the columns with a pair's tokens (four of each tile a lane): hides what a column does not see, and
   // raises the maxima where it has to.  ks: what the products are taken times for logits in powers of two
   __device__ __forceinline__ void hide(f32x4 (&s)[NQ][2], const int (&tok)[2]) {
@@ -225,26 +210,23 @@ struct Wave {
       }
     }
   }
-  // The weights, as the operand of the second product.  f: their factors (f16)
-  __device__ __forceinline__ void soften(const f32x4 (&s)[NQ][2], const float (&ks)[2], const float (&f)[2], uint4 (&w)[NQ]) {
+  // The weights, as operands of the second product: rounded, and what that left
+  __device__ __forceinline__ void soften(const f32x4 (&s)[NQ][2], const float (&ks)[2], uint4 (&w)[NQ][kParts]) {
 #pragma unroll
     for (int g = 0; g < NQ; ++g) {
       float pr[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][i >> 2][i & 3], ks[i >> 2], -m[g]));
       l[g] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-      u32 x[4];
+      u32 x[4], rest[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float p0 = pr[2 * i], p1 = pr[2 * i + 1];
-        if (!kPBf16) { p0 *= f[i >> 1]; p1 *= f[i >> 1]; }
-        x[i] = pack2<kPBf16>(p0, p1);
-        if (DUP) {
-          const u32 rest = pack2<true>(p0 - as_f32(x[i] << 16), p1 - as_f32(x[i] & 0xffff0000u));
-          x[i] = n & 8 ? rest : x[i];
-        }
+        x[i] = pack2<true>(pr[2 * i], pr[2 * i + 1]);
+        if (DUP || TWO) rest[i] = pack2<true>(pr[2 * i] - as_f32(x[i] << 16), pr[2 * i + 1] - as_f32(x[i] & 0xffff0000u));
+        if (DUP) x[i] = n & 8 ? rest[i] : x[i];
       }
-      w[g] = make_uint4(x[0], x[1], x[2], x[3]);
+      w[g][0] = make_uint4(x[0], x[1], x[2], x[3]);
+      if constexpr (TWO) w[g][1] = make_uint4(rest[0], rest[1], rest[2], rest[3]);
     }
   }
 
@@ -262,18 +244,18 @@ struct Wave {
       }
     }
     const float ks[2] = {a.scale_log2 * two_to(p.ek[0]), a.scale_log2 * two_to(p.ek[1])};
-    float f[2] = {1.f, 1.f};
-    if (!kPBf16) weigh(p.ev, f);
-    uint4 w[NQ];
+    uint4 w[NQ][kParts];
     hide(s, p.tok);
     raise(s, ks);
-    soften(s, ks, f, w);
-    const float v0 = kPBf16 ? two_to(p.ev[0]) : 1.f, v1 = kPBf16 ? two_to(p.ev[1]) : 1.f;
+    soften(s, ks, w);
+    const float v0 = two_to(p.ev[0]), v1 = two_to(p.ev[1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const auto v = widen<kPBf16>(word(p.v[0][i >> 2], i & 3), word(p.v[1][i >> 2], i & 3), v0, v1);
+      const bf16x8 v = widen<true>(word(p.v[0][i >> 2], i & 3), word(p.v[1][i >> 2], i & 3), v0, v1);
 #pragma unroll
-      for (int g = 0; g < NQ; ++g) o[g][i] = mfma32<kPBf16>(v, __builtin_bit_cast(typename Op<kPBf16>::type, w[g]), o[g][i]);
+      for (int x = 0; x < kParts; ++x)
+#pragma unroll
+        for (int g = 0; g < NQ; ++g) o[g][i] = mfma32<true>(v, __builtin_bit_cast(bf16x8, w[g][x]), o[g][i]);
     }
   }
 
@@ -282,7 +264,7 @@ struct Wave {
   template <class Lds>
   __device__ __forceinline__ void take_staged(const Lds& lds, int stage) {
     typedef typename Op<BF16>::type op;
-    op b[2][4];
+    uint4 b[2][4];
     // keys of tile 0 and 1, values of pair 0 in two halves, then the same of pair 1
     auto ask = [&](int i) {
 #pragma unroll
@@ -293,12 +275,11 @@ struct Wave {
     ask(0);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      int tok[2], ek[2], ev[2];
+      int tok[2], ek[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         tok[i] = __builtin_amdgcn_readfirstlane(lds.tok[stage][2 * x + i]);
         ek[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ek[stage][2 * x + i]);
-        ev[i] = BF16 ? 0 : __builtin_amdgcn_readfirstlane(lds.ev[stage][2 * x + i]);
       }
       f32x4 s[NQ][2];
 #pragma unroll
@@ -309,26 +290,27 @@ struct Wave {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(b[i][j], q[g][j], s[g][i]);
+          for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(__builtin_bit_cast(op, b[i][j]), q[g][j], s[g][i]);
       }
-      float ks[2] = {a.scale_log2, a.scale_log2}, f[2] = {1.f, 1.f};
+      float ks[2] = {a.scale_log2, a.scale_log2};
       if (!BF16) {
         ks[0] *= two_to(ek[0]);
         ks[1] *= two_to(ek[1]);
-        weigh(ev, f);
       }
       hide(s, tok);
       raise(s, ks);
-      uint4 w[NQ];
-      soften(s, ks, f, w);
+      uint4 w[NQ][kParts];
+      soften(s, ks, w);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (4 * x + i + 3 < 8) ask(4 * x + i + 3);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int g = 0; g < NQ; ++g)
-            o[g][i * 4 + j] = mfma32<BF16>(b[i][j], __builtin_bit_cast(op, w[g]), o[g][i * 4 + j]);
+          for (int y = 0; y < kParts; ++y)
+#pragma unroll
+            for (int g = 0; g < NQ; ++g)
+              o[g][i * 4 + j] = mfma32<true>(__builtin_bit_cast(bf16x8, b[i][j]), __builtin_bit_cast(bf16x8, w[g][y]), o[g][i * 4 + j]);
       }
     }
   }
@@ -413,11 +395,6 @@ struct Wave {
     for (int g = 0; g < NQ; ++g) {
       l[g] += __shfl_xor(l[g], 16, kWave);
       l[g] += __shfl_xor(l[g], 32, kWave);
-      if (!kPBf16) {
-        const float up = vref > -1000 ? two_to(vref - kLift) : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[g][i] *= up;
-      }
       if (DUP)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -442,8 +419,8 @@ __device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, in
 
 // Where a piece's result goes: to the output if it is all of the unit (count == 1), else to slot `mine` of the partial
 // results, which the last of the `count` pieces to arrive joins, in their order; slot(i) is the i-th one's number.
-template <bool BF16, int NQ, bool DUP, bool SEL>
-__device__ __forceinline__ void emit_wave(const AttnArgs& a, const Wave<BF16, NQ, DUP, SEL>& w) {
+template <bool BF16, int NQ, bool DUP, bool TWO, bool SEL>
+__device__ __forceinline__ void emit_wave(const AttnArgs& a, const Wave<BF16, NQ, DUP, TWO, SEL>& w) {
 #pragma unroll
   for (int g = 0; g < NQ; ++g) {
     int r, head;
@@ -456,8 +433,8 @@ __device__ __forceinline__ void emit_wave(const AttnArgs& a, const Wave<BF16, NQ
     }
   }
 }
-template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
-__device__ __forceinline__ void finish_wave(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, int count, int mine, int ticket, Slot slot) {
+template <bool BF16, int NQ, bool DUP, bool TWO, bool SEL, class Slot>
+__device__ __forceinline__ void finish_wave(const AttnArgs& a, Wave<BF16, NQ, DUP, TWO, SEL>& w, int count, int mine, int ticket, Slot slot) {
   if (count > 1) {
     w.leave(mine);                             // (written through and drained before the ticket, and read past the caches: no fence
     wave_drain_memory();                       // of the ticket's, which would empty an XCD's L2: 583 us for 533 with it)
@@ -479,8 +456,8 @@ struct AttnLds {
 };
 
 // The waves' results of one unit as one: with to_slot < 0 to the output, else there
-template <bool BF16, int NQ, bool DUP, bool SEL>
-__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, int to_slot) {
+template <bool BF16, int NQ, bool DUP, bool TWO, bool SEL>
+__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, NQ, DUP, TWO, SEL>& w, AttnLds<NQ>& lds, int to_slot) {
   const int tid = threadIdx.x, wave = tid / kWave;
   __syncthreads();                             // (what was there has been read)
 #pragma unroll
@@ -531,8 +508,8 @@ __device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, 
   }
 }
 // The same as finish_wave for a piece that the waves of the workgroup shared
-template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
-__device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, int count, int mine,
+template <bool BF16, int NQ, bool DUP, bool TWO, bool SEL, class Slot>
+__device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, DUP, TWO, SEL>& w, AttnLds<NQ>& lds, int count, int mine,
                                              int ticket, Slot slot) {
   merge_waves(a, w, lds, count == 1 ? -1 : mine);
   if (count == 1) return;
@@ -549,8 +526,8 @@ __device__ __forceinline__ void finish_group(const AttnArgs& a, Wave<BF16, NQ, D
 }
 
 // Tiles [t0, t1) of a unit: by all waves, or, a short unit, by wave `solo` alone.
-template <bool BF16, int NQ, bool DUP, bool SEL, class Slot>
-__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, DUP, SEL>& w, AttnLds<NQ>& lds, const Unit& u, int t0, int t1,
+template <bool BF16, int NQ, bool DUP, bool TWO, bool SEL, class Slot>
+__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, DUP, TWO, SEL>& w, AttnLds<NQ>& lds, const Unit& u, int t0, int t1,
                                       int solo, int count, int mine, int ticket, Slot slot) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (!SEL) t1 = min(t1, max(t0, (u.pos0 + u.rows - 1) / kTile + 1));   // none of the rows sees more
@@ -678,11 +655,11 @@ __device__ __forceinline__ void deal(const AttnArgs& a, bool grow, Each each) {
 
 // A few rows of a sequence (up to 16 NQ columns): each wave has all of them and a part of the tokens, with a pair of tiles on its
 // way behind the one it takes.  Bound by the memory: 16 x 32768 tokens of 8 heads 167 us (6.4 TB/s), 24 ragged contexts with up to
-// three rows of 7 x 4 heads 103 us (5.2 TB/s); short contexts by their chain of trips to memory (4 x 1000 tokens 14.5 us).
+// three rows of 7 x 4 heads 105 us (5.1 TB/s); short contexts by their chain of trips to memory (4 x 1000 tokens 14.5 us).
 template <bool BF16, int NQ, bool DUP>
 __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs a) {
   __shared__ AttnLds<NQ> lds;
-  Wave<BF16, NQ, DUP, false> w(a);
+  Wave<BF16, NQ, DUP, !DUP, false> w(a);
   int solo = 0;
   deal<kAttnThreads>(a, false, [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
     piece(a, w, lds, u, t0, t1, solo, count, mine, f, slot);
@@ -698,20 +675,18 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs
 // (800), with 32 a widened code serves fewer columns, but all fits.
 constexpr int kRowGroups = 2;
 constexpr int kStageTiles = kAttnWaves;
-template <bool BF16>
 struct RowsLds {
-  typedef typename Op<BF16>::type op;
-  op k[2][kStageTiles][4][kWave];              // [stage][tile][32 elements][lane]
-  op v[2][kStageTiles / 2][8][kWave];          // [stage][pair of tiles][16 elements][lane]
-  int tok[2][kStageTiles], ek[2][kStageTiles], ev[2][kStageTiles];
+  uint4 k[2][kStageTiles][4][kWave];           // [stage][tile][32 elements][lane], in the type of q
+  uint4 v[2][kStageTiles / 2][8][kWave];       // [stage][pair of tiles][16 elements][lane], in bf16
+  int tok[2][kStageTiles], ek[2][kStageTiles];
 };
 
 template <bool BF16>
 __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs a) {
   constexpr int NQ = kRowGroups;
-  __shared__ RowsLds<BF16> lds;
+  __shared__ RowsLds lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  Wave<BF16, NQ, false, false> w(a);
+  Wave<BF16, NQ, false, !BF16, false> w(a);
   const int tpp = a.P / kTile, rows = a.R / kAttnWaves;                // tiles of a page; rows of a wave
   deal<kAttnThreads>(a, true, [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
@@ -752,19 +727,19 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
       if (tok == kNowhere)
 #pragma unroll
         for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
-      // (bf16 has the range to take the scales in; f16 has not, and theirs go into the logits and the weights)
-      const float sk = BF16 ? two_to(ek) : 1.f, sv = BF16 ? two_to(ev) : 1.f;
+      // (bf16 has the range to take the keys' scale in; f16 has not, and it goes into the logits)
+      const float sk = BF16 ? two_to(ek) : 1.f, sv = two_to(ev);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        lds.k[s][wave][j][w.lane] = widen<BF16>(word(raw[j >> 1], (j & 1) * 2), word(raw[j >> 1], (j & 1) * 2 + 1), sk, sk);
+        lds.k[s][wave][j][w.lane] = __builtin_bit_cast(uint4, widen<BF16>(word(raw[j >> 1], (j & 1) * 2), word(raw[j >> 1], (j & 1) * 2 + 1), sk, sk));
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        const uint4 x = __builtin_bit_cast(uint4, widen<BF16>(word(raw[2 + (i >> 2)], i & 3), word(raw[2 + (i >> 2)], (i & 3) + 1), sv, sv));
+        const uint4 x = __builtin_bit_cast(uint4, widen<true>(word(raw[2 + (i >> 2)], i & 3), word(raw[2 + (i >> 2)], (i & 3) + 1), sv, sv));
         u64* to = reinterpret_cast<u64*>(&lds.v[s][wave >> 1][i][w.lane]) + (wave & 1);
         to[0] = (u64)x.y << 32 | x.x;
         to[2 * kWave] = (u64)x.w << 32 | x.z;  // (the next 16 elements' operand)
       }
-      if (w.lane == 0) { lds.tok[s][wave] = tok; lds.ek[s][wave] = ek; lds.ev[s][wave] = ev; }
+      if (w.lane == 0) { lds.tok[s][wave] = tok; lds.ek[s][wave] = ek; }
     };
     __syncthreads();                           // (the last piece's stages have been read)
     if (t0 < t1) {
@@ -802,7 +777,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_selected_kernel(AttnA
   if ((unsigned)u.seq >= (unsigned)a.B || u.pos0 < 0 || u.pos0 >= a.NP * a.P) return;
   u.entries = min(a.k, u.pos0 / a.P + 1);
   const int tiles = u.entries * (a.P / kTile), per = (tiles + a.S - 1) / a.S;
-  Wave<BF16, 1, true, true> w(a);
+  Wave<BF16, 1, true, false, true> w(a);
   piece(a, w, lds, u, min(s * per, tiles), min((s + 1) * per, tiles), 0, a.S, unit * a.S + s, unit,
         [&](int x) { return unit * a.S + x; });
 }
