@@ -5,9 +5,14 @@
 // product.  Tiles come from memory in operand order, 16 bytes a lane and load; codes become 16-bit numbers in registers, which
 // holds every e4m3 value exactly.  The keys' scale goes into the logits, the values' into the conversion.
 //
-// One pass with a running maximum m and sum l of a column: p = 2^(x - m).  m is raised only when a logit passes it by
-// more than kSlack, so that the accumulators are rarely touched; p then stays below 2^kSlack, and nothing is lost, as all of this
-// is floating point.
+// One pass with a running reference m and sum l of a column: p = 2^(x - m).  m is kHead above the largest logit when it is set, and
+// is raised only when a logit passes that by more than kSlack, so that the accumulators are rarely touched; p then stays below
+// 2^(kSlack - kHead), and nothing is lost, as all of this is floating point.
+//
+// Nothing is infinite on the way either.  The largest value, 448 * 2^120, is beyond fp32; one that became an infinity would make NaN of
+// every hidden weight of 0 too.  Values are taken times 2^-kValueDown, which leaves the least, 2^-105, a normal number; weights
+// are below 2^-4, so that the sum of 2^24 tokens is below 2^(24 - 4 + 129 - 21) = 2^128.  Keys that are widened with their scale
+// are taken times 2^-kKeyDown.
 //
 // Weights and values go to the second product in bf16, which has the range for any scale of a page: no page's scale, seen or
 // hidden, costs another page's tokens anything.  (f16 has not: weights relative to the largest scale of a wave's pages lost
@@ -29,7 +34,8 @@ constexpr int kCoopTiles = 8;                  // from so many tiles on a unit i
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 // 8-byte words of a wave's partial result: accumulators, then a maximum and a sum a column
 __host__ __device__ constexpr size_t part_words(int groups) { return (size_t)groups * (16 * kWave + 16); }
-constexpr float kLowest = -3.0e38f, kSlack = 8.f;
+constexpr float kLowest = -3.0e38f, kSlack = 8.f, kHead = 12.f;
+constexpr int kValueDown = 21, kKeyDown = 2;
 constexpr int kNowhere = 1 << 30;              // position of a tile that no row sees
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -194,7 +200,7 @@ struct Wave {
     for (int g = 0; g < NQ; ++g) {             // (ks > 0 keeps the order)
       mx[g] = fmaxf(fmaxf(max3(s[g][0][0], s[g][0][1], s[g][0][2]), s[g][0][3]) * ks[0],
                     fmaxf(max3(s[g][1][0], s[g][1][1], s[g][1][2]), s[g][1][3]) * ks[1]);
-      any |= mx[g] > m[g] + kSlack;
+      any |= mx[g] > m[g] - (kHead - kSlack);
     }
     if (__any(any)) {
 #pragma unroll
@@ -202,7 +208,7 @@ struct Wave {
         mx[g] = fmaxf(mx[g], __shfl_xor(mx[g], 16, kWave));
         mx[g] = fmaxf(mx[g], __shfl_xor(mx[g], 32, kWave));
         // (a column that does not need it stays, so that no row's result depends on its neighbours)
-        const float to = mx[g] > m[g] + kSlack ? mx[g] : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
+        const float to = mx[g] > m[g] - (kHead - kSlack) ? mx[g] + kHead : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
         m[g] = to;
         l[g] *= down;
 #pragma unroll
@@ -248,7 +254,7 @@ struct Wave {
     hide(s, p.tok);
     raise(s, ks);
     soften(s, ks, w);
-    const float v0 = two_to(p.ev[0]), v1 = two_to(p.ev[1]);
+    const float v0 = two_to(p.ev[0] - kValueDown), v1 = two_to(p.ev[1] - kValueDown);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const bf16x8 v = widen<true>(word(p.v[0][i >> 2], i & 3), word(p.v[1][i >> 2], i & 3), v0, v1);
@@ -292,11 +298,9 @@ struct Wave {
 #pragma unroll
           for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(__builtin_bit_cast(op, b[i][j]), q[g][j], s[g][i]);
       }
-      float ks[2] = {a.scale_log2, a.scale_log2};
-      if (!BF16) {
-        ks[0] *= two_to(ek[0]);
-        ks[1] *= two_to(ek[1]);
-      }
+      float ks[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) ks[i] = a.scale_log2 * two_to(BF16 ? kKeyDown : ek[i]);
       hide(s, tok);
       raise(s, ks);
       uint4 w[NQ][kParts];
@@ -408,7 +412,7 @@ struct Wave {
 template <bool BF16, int N>
 __device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, int head, int d, const float (&v)[N], float m, float l) {
   const size_t at = (size_t)(u.row0 + r) * a.H * a.G + u.h * a.G + head;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = l == 0.f ? 0.f : two_to(kValueDown) / l;
   u32 w[N / 2];
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) w[i] = pack2<BF16>(l == 0.f ? 0.f : v[2 * i] * inv, l == 0.f ? 0.f : v[2 * i + 1] * inv);
@@ -728,7 +732,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
 #pragma unroll
         for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
       // (bf16 has the range to take the keys' scale in; f16 has not, and it goes into the logits)
-      const float sk = BF16 ? two_to(ek) : 1.f, sv = two_to(ev);
+      const float sk = BF16 ? two_to(ek - kKeyDown) : 1.f, sv = two_to(ev - kValueDown);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         lds.k[s][wave][j][w.lane] = __builtin_bit_cast(uint4, widen<BF16>(word(raw[j >> 1], (j & 1) * 2), word(raw[j >> 1], (j & 1) * 2 + 1), sk, sk));

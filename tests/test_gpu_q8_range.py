@@ -68,3 +68,69 @@ def test_a_visible_page_of_large_values_and_no_weight_costs_the_others_nothing(l
         # (2^-100 of 2^16 is nothing)
         got = out[row].double().cpu().numpy()
         assert (np.abs(got - o) <= tol).all(), (row, np.abs(got - o).max(), tol.min())
+
+
+# ---- the top of the range: magnitudes above 448 * 2^119, whose codes stand for numbers up to 448 * 2^120
+
+@pytest.mark.parametrize("lens,news", [([1000], [1])] + SPLIT)
+def test_values_at_the_top_of_the_range_are_numbers(lens, news):
+    """bf16: every value of the second page of a pair, which the first rows do not see, is of the largest scale."""
+    s = Step(lens, news, H=2, seed=41)
+    block = int(s.table[0, (lens[0] // 16 + 1) if news[0] > 1 else 5])
+    s.cache.exps[block, :, 1] = 120
+    q = s.query(0.25)
+    s.check_attention(q, *s.attend(q))
+
+
+@pytest.mark.parametrize("lens,news", SPLIT)
+def test_hidden_keys_at_the_top_of_the_range_reach_nothing(lens, news):
+    s = Step(lens, news, H=2, seed=42)
+    s.cache.exps[int(s.table[0, lens[0] // 16 + 1])] = 120
+    q = s.query(0.25)
+    before = [r for r in range(s.real) if s.pos[r] // 16 == lens[0] // 16]
+    s.check_attention(q, *s.attend(q), rows=before)
+
+
+@pytest.mark.parametrize("lens,news", [([70000], [1]), ([70000], [2]), ([9000], [6]), ([6000], [40])])
+@pytest.mark.parametrize("growing", [False, True])
+def test_sums_of_many_values_at_the_top_of_the_range_are_numbers(lens, news, growing):
+    """Every value is between 104 and 240 times 2^120, that is below bf16's largest number, and so is their mean; with `growing` all
+    tokens but the first few have e^5 times the weight of those, which is when weights are largest."""
+    s = Step(lens, news, H=1, seed=43)
+    s.cache.exps[:, :, 1] = 120
+    _, val = R.tile_places(16)
+    at = torch.from_numpy(val.ravel()).to(G.DEV)
+    flat = s.cache.pages.view(s.NB, s.H, -1)
+    flat[:, :, at] = torch.randint(0x6D, 0x78, (s.NB, s.H, at.numel()), generator=s.gen, device=G.DEV, dtype=torch.uint8)
+    q = s.query(0.1)
+    if growing:
+        key, _ = R.tile_places(16)
+        s.cache.exps[:, :, 0] = -5
+        q[..., 0] = 4.0
+        flat[:, :, torch.from_numpy(key[:, 0]).to(G.DEV)] = 0x7E                            # 448 * 2^-5: logits of 4.95
+        flat[int(s.table[0, 0])][:, torch.from_numpy(key[:, 0]).to(G.DEV)] = 0
+    out, lse = s.attend(q)
+    ref = G.to_ref(s.cache, s.P)
+    for row in range(0, s.real, 5):
+        o, l, tol = _bound(s, ref, row, 0, q, 1.0 / math.sqrt(D), 2.0 ** -8)
+        got = out[row].double().cpu().numpy()
+        assert (np.abs(got - o) <= tol).all(), (row, got.max(), o.max())
+
+
+@pytest.mark.parametrize("news", [[40], [1]])
+def test_what_is_appended_at_the_ends_of_the_range_is_attended_to(news):
+    """Tokens with bf16's largest number, with infinities and NaN beside it, behind ordinary ones."""
+    s = Step([0] if news[0] > 1 else [39], news, H=2, seed=44)
+    s.cache.exps.zero_()
+    top = torch.finfo(torch.bfloat16).max
+    T = 40
+    full = s if news[0] > 1 else Step([0], [40], H=2, seed=44)
+    k, v = full.randn(T, 2, D), full.randn(T, 2, D)
+    v[20, 0, 3], v[21, 0, 4], v[22, 0, 5], v[39, 1, 7] = top, float("inf"), float("nan"), -top
+    full.cache.append(full.rows, k, v)
+    if full is not s:
+        for b, c in zip(s.table[0], full.table[0]):
+            for name in ("pages", "exps"):
+                getattr(s.cache, name)[int(b)] = getattr(full.cache, name)[int(c)]
+    q = s.query(0.25)
+    s.check_attention(q, *s.attend(q))
