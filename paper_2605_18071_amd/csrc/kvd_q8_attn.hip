@@ -180,8 +180,14 @@ struct Wave {
     }
   }
 
+  // What products with keys of scale 2^e are taken times for logits in powers of two.  Never 0, which would make NaN of a hidden
+  // product's -infinity (what that adds to a logit is below 2^-126 of its product), nor infinite, which would make it of a product
+  // that is 0.
+  __device__ __forceinline__ float logit_scale(int e) const {
+    return __builtin_amdgcn_fmed3f(a.scale_log2 * two_to(e), 0x1p-126f, 0x1.fffffep127f);
+  }
   // The products q k of the columns with a pair's tokens (four of each tile a lane): hides what a column does not see, and
-  // raises the maxima where it has to.  ks: what the products are taken times for logits in powers of two
+  // raises the maxima where it has to.  ks: their logit_scale
   __device__ __forceinline__ void hide(f32x4 (&s)[NQ][2], const int (&tok)[2]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -249,7 +255,7 @@ struct Wave {
         for (int g = 0; g < NQ; ++g) s[g][i] = mfma32<BF16>(k, q[g][j], s[g][i]);
       }
     }
-    const float ks[2] = {a.scale_log2 * two_to(p.ek[0]), a.scale_log2 * two_to(p.ek[1])};
+    const float ks[2] = {logit_scale(p.ek[0]), logit_scale(p.ek[1])};
     uint4 w[NQ][kParts];
     hide(s, p.tok);
     raise(s, ks);
@@ -300,7 +306,7 @@ struct Wave {
       }
       float ks[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) ks[i] = a.scale_log2 * two_to(BF16 ? kKeyDown : ek[i]);
+      for (int i = 0; i < 2; ++i) ks[i] = logit_scale(BF16 ? kKeyDown : ek[i]);
       hide(s, tok);
       raise(s, ks);
       uint4 w[NQ][kParts];

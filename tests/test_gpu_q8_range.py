@@ -134,3 +134,27 @@ def test_what_is_appended_at_the_ends_of_the_range_is_attended_to(news):
                 getattr(s.cache, name)[int(b)] = getattr(full.cache, name)[int(c)]
     q = s.query(0.25)
     s.check_attention(q, *s.attend(q))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("scale,exp", [(1e-25, R.EXP_MIN), (1e6, 120)])
+@pytest.mark.parametrize("lens,news", [([0], [1]), ([1000], [1])] + SPLIT)
+def test_scales_that_leave_nothing_of_the_logits(dtype, scale, exp, lens, news):
+    """softmax_scale = 1e-25 beside keys of the least scale (as pages of zeros have it), or 1e6 beside those of the largest and queries
+    of 0: every logit is 0 in 32 bits, and every row the mean of the values that it sees.  All weights are the same power of two,
+    so that an output is off by half a step of its type, 2^-17 of A for the sums, and what rounding 1/l costs."""
+    s = Step(lens, news, dtype=dtype, H=2, seed=51, softmax_scale=scale)
+    for page in (0, (lens[0] + news[0] - 1) // 16):
+        s.cache.exps[int(s.table[0, page]), :, 0] = exp
+    q = s.query(1.0 if scale < 1.0 else 0.0)
+    out, lse = s.attend(q)
+    ref = G.to_ref(s.cache, s.P)
+    h = torch.finfo(G.torch_type(dtype)).eps / 2
+    for row in range(s.real):
+        n = s.pos[row] + 1
+        for head in range(s.H):
+            _, v = ref.kv(s.table[0][: (n - 1) // 16 + 1], head)
+            o, A = v[:n].mean(0), np.abs(v[:n]).mean(0)
+            got = out[row, head * s.G:(head + 1) * s.G].double().cpu().numpy()
+            assert (np.abs(got - o) <= h * np.abs(o) + 2.0 ** -16 * A + (2.0 ** -25 if dtype == "f16" else 0.0)).all(), (row, head)
+            assert np.abs(lse[row, head * s.G:(head + 1) * s.G].cpu().numpy() - math.log(n)).max() <= 2.0 ** -20 * (1 + math.log(n)), (row, head)
