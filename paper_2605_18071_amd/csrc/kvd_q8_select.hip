@@ -149,9 +149,9 @@ __global__ __launch_bounds__(kScoreThreads, 4) void q8_score_kernel(SelectArgs a
   }
 }
 
-// Scores as whole numbers of the same order; -0 does not occur (a product is 0 or at least 2^-126 in magnitude)
+// Scores as whole numbers of the same order; -0, which a scale of 0 makes of a negative product, is 0
 __device__ __forceinline__ u32 order_of(float s) {
-  const u32 b = as_u32(s);
+  const u32 b = as_u32(s + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 

@@ -158,3 +158,16 @@ def test_scales_that_leave_nothing_of_the_logits(dtype, scale, exp, lens, news):
             got = out[row, head * s.G:(head + 1) * s.G].double().cpu().numpy()
             assert (np.abs(got - o) <= h * np.abs(o) + 2.0 ** -16 * A + (2.0 ** -25 if dtype == "f16" else 0.0)).all(), (row, head)
             assert np.abs(lse[row, head * s.G:(head + 1) * s.G].cpu().numpy() - math.log(n)).max() <= 2.0 ** -20 * (1 + math.log(n)), (row, head)
+
+
+# ---- scores
+
+@pytest.mark.parametrize("pages", [60, 1500])
+def test_scores_of_minus_zero_are_those_of_zero(pages):
+    """Pages whose scale is 0 score 0 whatever the sign of their product: a tie, which the lower page wins."""
+    s = Step([pages * 16 - 2], [1], H=2, seed=61)
+    s.cache.mean_scales.zero_()
+    q = s.query()
+    sel = torch.full((1, s.H, 9), -9, dtype=torch.int32, device=G.DEV)
+    s.cache.select(s.rows, q, sel, s.cache.workspace(s.rows, select=True))
+    assert sel.cpu().tolist() == [[list(range(9))] * s.H]
