@@ -530,8 +530,9 @@ typedef struct {
  *   free_blocks [n_free] with *free_count (device) valid entries, taken from the last one down: first for the first
  *   sequence, in page order.
  * Writes the page-table entries of the pages that are begun (no others), and everything else in rows.  min(T, T/P + 2B)
- * runs are always enough.  The inputs stay as they are: the caller takes counts[3] for the next step's free_count.  If the
- * step does not fit, counts[4] says why, and it has no rows, no runs and no new blocks (kv_len = seq_len).
+ * runs are always enough.  The inputs stay as they are: for the next step the caller copies kv_len to seq_len and counts[3] to
+ * free_count.  The inputs must be other memory than rows' buffers, as some workgroups read them while others write those; kv_len as
+ * seq_len or n_new and counts + 3 as free_count are refused (KVD_ERR_ARG).  If the step does not fit, counts[4] says why, and it has no rows, no runs and no new blocks (kv_len = seq_len).
  * A last page that is partly filled is continued in place: it must not be shared with another sequence. */
 int kvd_q8_map(const kvd_q8_rows* rows, const int32_t* seq_len, const int32_t* n_new, const int32_t* free_blocks,
                int32_t n_free, const int32_t* free_count, void* stream);

@@ -591,7 +591,8 @@ class Q8Rows(_OnDevice):
         self._ref = C.byref(self.c)
 
     def map(self, seq_len: torch.Tensor, n_new: torch.Tensor, free_blocks: torch.Tensor, free_count: torch.Tensor, stream=None):
-        """kvd_q8_map: the step that adds n_new tokens to sequences of seq_len."""
+        """kvd_q8_map: the step that adds n_new tokens to sequences of seq_len.  For the next step copy kv_len to seq_len and
+        counts[3:4] to free_count: the inputs must not be this object's own buffers."""
         _buffer("seq_len", seq_len, (self.n_seqs,), torch.int32, self.device)
         _buffer("n_new", n_new, (self.n_seqs,), torch.int32, self.device)
         _buffer("free_blocks", free_blocks, (free_blocks.numel(),), torch.int32, self.device)
