@@ -505,7 +505,8 @@ typedef struct {
   float* mean_scales;      /* [NB][Hkv] */
 } kvd_q8_cache;
 
-/* A step's rows.  Written by kvd_q8_map and read by the other calls; a caller may also fill them itself. */
+/* A step's rows.  Written by kvd_q8_map and read by the other calls; a caller may also fill them itself.  kvd_q8_append reads
+ * runs, kvd_q8_select page_table, row_seq and row_pos, kvd_q8_attn all but runs and counts. */
 typedef struct {
   int32_t n_seqs;          /* B */
   int32_t max_pages;       /* NP */

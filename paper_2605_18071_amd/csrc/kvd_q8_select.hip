@@ -18,7 +18,7 @@ constexpr int kSelectThreads = 1024;
 struct SelectArgs {
   const uint16_t* q;
   long long q_stride;
-  const int32_t *table, *row_start, *row_seq, *row_pos;
+  const int32_t *table, *row_seq, *row_pos;
   const int8_t* means;
   const float* mean_scales;
   float* scores;                               // [T][H][NP]
@@ -34,7 +34,7 @@ __device__ __forceinline__ int pages_seen(const SelectArgs& a, int r, int& seq) 
   return pos / a.P + 1;
 }
 
-// One workgroup: 16 rows of a sequence and HG heads, PW pages a wave and step (64, and less where that would leave CUs without
+// One workgroup: up to 16 rows of a sequence and HG heads, PW pages a wave and step (64, and less where that would leave CUs without
 // work: 12 x 4 rows of 938 pages take 15 us with 64).  A load takes the entries of all these heads from one
 // page (8 lanes of 16 bytes a head): they are neighbours in memory, and a load whose lanes went to 16 pages, as operands of the
 // matrix cores would have it, went at 3.1 TB/s instead of 4.1 (45 us instead of 34 for 16 x 8192 pages of 8 heads).
@@ -49,11 +49,12 @@ __global__ __launch_bounds__(kScoreThreads, 4) void q8_score_kernel(SelectArgs a
   const int span = a.span * kScorePages;       // pages of this workgroup
   const int r0 = blockIdx.x, h0 = blockIdx.y * HG, p0 = blockIdx.z * span;
   const bool head = h0 + x < a.H;
-  // rows r0 .. r0 + 15, as far as they are of one sequence; lanes 16 apart have the same
+  // rows r0 .. up to the next multiple of 16, as far as they are of one sequence; lanes 16 apart have the same
   const int n = lane & 15, r = min(r0 + n, a.T - 1), row_seq = a.row_seq[r], row_pos = a.row_pos[r];
+  const int before = r0 % kScoreRows ? a.row_seq[r0 - 1] : -1;
   const int seq = __builtin_amdgcn_readfirstlane(row_seq);
   if ((unsigned)seq >= (unsigned)a.B) return;
-  const bool mine = row_seq == seq && r0 + n < a.T && row_pos >= 0 && row_pos < a.NP * a.P;
+  const bool mine = row_seq == seq && r0 % kScoreRows + n < kScoreRows && r0 + n < a.T && row_pos >= 0 && row_pos < a.NP * a.P;
   const int seen = mine ? row_pos / a.P + 1 : 0;
   int most = seen;
 #pragma unroll
@@ -61,13 +62,11 @@ __global__ __launch_bounds__(kScoreThreads, 4) void q8_score_kernel(SelectArgs a
   most = __builtin_amdgcn_readfirstlane(most);
   if (p0 >= most) return;
   const int np = min(most - p0, span);
-  // (this workgroup is for rows 0, 16, 32, ... of a sequence)
-  const int back = r0 - a.row_start[seq];
   const int32_t* table = a.table + (size_t)seq * a.NP + p0;
   auto blocks_of = [&](int at) { return lane < PW && at + lane < np ? table[at + lane] : -1; };   // of the wave's pages from `at` on
   int at = w * PW;
   int blk = blocks_of(at);
-  if (back < 0 || back % kScoreRows != 0) return;
+  if (before == seq) return;                   // (an earlier row's workgroup has this one, too)
   // the queries in 8 bits: a wave a row and head, two elements a lane
   for (int i = w; i < kScoreRows * HG; i += kScoreThreads / kWave) {
     const int row = i / HG, y = i % HG;
@@ -305,11 +304,11 @@ extern "C" int kvd_q8_select(const kvd_q8_cache* c, const kvd_q8_rows* r, const 
   if (topk_pages < 1 || topk_pages > KVD_MAX_TOPK || !stride_ok(q_stride, c->n_q_heads)) return KVD_ERR_SHAPE;
   if ((int64_t)c->sink_pages + c->recent_pages > topk_pages) return KVD_ERR_CAPACITY;
   if (!aligned(c->means, 16) || !aligned(c->mean_scales, 4) || !aligned(q, 16) || !aligned(sel_pages, 4) || !aligned(workspace, 16)) return KVD_ERR_ARG;
-  if (!aligned(r->page_table, 4) || !aligned(r->row_start, 4) || !aligned(r->row_seq, 4) || !aligned(r->row_pos, 4)) return KVD_ERR_ARG;
+  if (!aligned(r->page_table, 4) || !aligned(r->row_seq, 4) || !aligned(r->row_pos, 4)) return KVD_ERR_ARG;
   if (workspace_bytes < kvd_q8_select_bytes(c, r)) return KVD_ERR_CAPACITY;
   SelectArgs a;
   a.q = static_cast<const uint16_t*>(q); a.q_stride = q_stride;
-  a.table = r->page_table; a.row_start = r->row_start; a.row_seq = r->row_seq; a.row_pos = r->row_pos;
+  a.table = r->page_table; a.row_seq = r->row_seq; a.row_pos = r->row_pos;
   a.means = c->means; a.mean_scales = c->mean_scales;
   a.scores = reinterpret_cast<float*>(static_cast<char*>(workspace) + kTicketBytes); a.sel = sel_pages;
   a.B = r->n_seqs; a.NP = r->max_pages; a.T = r->n_rows; a.H = c->n_kv_heads; a.G = c->n_q_heads / c->n_kv_heads;

@@ -171,3 +171,20 @@ def test_scores_of_minus_zero_are_those_of_zero(pages):
     sel = torch.full((1, s.H, 9), -9, dtype=torch.int32, device=G.DEV)
     s.cache.select(s.rows, q, sel, s.cache.workspace(s.rows, select=True))
     assert sel.cpu().tolist() == [[list(range(9))] * s.H]
+
+
+@pytest.mark.parametrize("H,lens,news", [(2, [900, 0, 333], [1, 3, 20]), (5, [400] * 9, [1, 2, 3, 16, 17, 1, 40, 1, 5])])
+def test_selection_needs_sequences_and_positions_of_the_rows_only(H, lens, news):
+    """Rows that a caller has filled without kv_len and row_start, with another selection's scores in the workspace."""
+    s = Step(lens, news, H=H, seed=62)
+    ws = s.cache.workspace(s.rows, select=True)
+    want, got = (torch.full((s.T, H, 7), -9, dtype=torch.int32, device=G.DEV) for _ in range(2))
+    q = s.query()
+    s.cache.select(s.rows, q, want, ws)
+    s.rows.row_start.fill_(10 ** 6)
+    s.rows.kv_len.zero_()
+    s.cache.select(s.rows, -q, got, ws)
+    ref, qd = G.to_ref(s.cache, s.P), -q.double().cpu().numpy()
+    for r in range(s.real):
+        for h in range(H):
+            assert got[r, h].tolist() == R.select_row(ref, s.table[s.seq[r]], qd[r, h * s.G:(h + 1) * s.G], h, s.pos[r], 7, 0, 0, s.NB), (r, h)
