@@ -2,7 +2,8 @@
 // head.  The largest magnitude gives the scale 2^e, the elements times 2^-e go to e4m3 by the hardware's conversion,
 // which rounds to nearest even; products with powers of two are exact, so that there is no rounding but that one.  Codes are
 // put together in LDS, so that the pool is written 16 bytes a lane.  Bound by the memory: 4 bytes read and
-// 2 written for an element of a key and its value's (32768 tokens of 8 heads 44 us, 4.6 TB/s; a token for each of 64 requests 5.3).
+// 2 written for an element of a key and its value's (32768 tokens of 8 heads 44 us, 4.6 TB/s, and 50 where the card has run for
+// long; a token for each of 64 requests 5.2).
 #include "kvd_q8.h"
 
 namespace kvd {

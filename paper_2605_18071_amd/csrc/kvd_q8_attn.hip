@@ -665,7 +665,7 @@ __device__ __forceinline__ void deal(const AttnArgs& a, bool grow, Each each) {
 
 // A few rows of a sequence (up to 16 NQ columns): each wave has all of them and a part of the tokens, with a pair of tiles on its
 // way behind the one it takes.  Bound by the memory: 16 x 32768 tokens of 8 heads 167 us (6.4 TB/s), 24 ragged contexts with up to
-// three rows of 7 x 4 heads 105 us (5.1 TB/s); short contexts by their chain of trips to memory (4 x 1000 tokens 14.5 us).
+// three rows of 7 x 4 heads 104 us (5.1 TB/s); short contexts by their chain of trips to memory (4 x 1000 tokens 14.5 us).
 template <bool BF16, int NQ, bool DUP>
 __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs a) {
   __shared__ AttnLds<NQ> lds;
@@ -680,7 +680,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs
 // Many rows of a sequence: each wave has its own kRowGroups * 16 columns, and the workgroup goes through the tokens together,
 // 64 at a time: every wave fetches one tile, widens it and puts it into LDS in operand order, while the 64 before it are
 // taken; so a code is widened once for four waves.  Bound by the matrix cores and the vector unit alike, which two waves a SIMD hardly
-// get to work at the same time: 2 x 2048 rows of 32/8 heads behind 6144 tokens 533 us (900 TFLOP/s).  With 48 columns a wave
+// get to work at the same time: 2 x 2048 rows of 32/8 heads behind 6144 tokens 530 us (910 TFLOP/s).  With 48 columns a wave
 // registers spill (818 us), with 64 and a SIMD's registers for one wave the vector unit's values land in accumulation registers
 // (800), with 32 a widened code serves fewer columns, but all fits.
 constexpr int kRowGroups = 2;
@@ -773,7 +773,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
 }
 
 // Selected pages: a unit is one row and head, in S pieces, so that there are two workgroups for each CU.  16 x 8 units of 256 pages
-// 30 us (4.5 TB/s): the memory behind a chain of selection, table, exponents and pages.
+// 29 us (4.6 TB/s): the memory behind a chain of selection, table, exponents and pages.
 template <bool BF16>
 __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_selected_kernel(AttnArgs a) {
   __shared__ AttnLds<1> lds;

@@ -1,7 +1,7 @@
 // Page tables and slot maps of a step, built on the GPU from the requests' lengths: three prefix sums over the
 // sequences (rows, runs, pages begun), then every row, run and new page finds its sequence in them by bisection.
-// Everything is a few bytes an item: the time is the launch and a handful of dependent trips to memory and LDS (6.5 us for 256
-// sequences with a row each and for 96 with 54000 rows).
+// Everything is a few bytes an item: the time is the launch and a handful of dependent trips to memory and LDS (6.4 us for 256
+// sequences with a row each, 7.3 for 96 with 54000 rows).
 // Every workgroup makes the sums for itself (the lengths come out of L2, which is less than a second launch), and
 // writes a slice of the items.
 #include "kvd_q8.h"

@@ -1,6 +1,7 @@
 // Selection of pages by a score in 8 bits.  Two launches: the scores of all visible pages of every row and head, as
 // products of whole numbers (int8, exact, so that the result does not depend on the order), and the k best
-// of a row and head by one workgroup, which holds the scores in registers.  Scoring is bound by the memory (132 bytes a page and
+// of a row and head by one workgroup, which holds the scores in registers (a table of more than 16384 pages has 64 a
+// thread, of which the compiler spills about half).  Scoring is bound by the memory (132 bytes a page and
 // head), selecting by its trips to LDS.
 #include <type_traits>
 
@@ -37,7 +38,7 @@ __device__ __forceinline__ int pages_seen(const SelectArgs& a, int r, int& seq) 
 // One workgroup: up to 16 rows of a sequence and HG heads, PW pages a wave and step (64, and less where that would leave CUs without
 // work: 12 x 4 rows of 938 pages take 15 us with 64).  A load takes the entries of all these heads from one
 // page (8 lanes of 16 bytes a head): they are neighbours in memory, and a load whose lanes went to 16 pages, as operands of the
-// matrix cores would have it, went at 3.1 TB/s instead of 4.1 (45 us instead of 34 for 16 x 8192 pages of 8 heads).
+// matrix cores would have it, went at 3.1 TB/s instead of 4.5 (31 us for 16 x 8192 pages of 8 heads).
 // The products are few enough for the vector unit: four elements an instruction.
 template <bool BF16, int HG, int PW>
 __global__ __launch_bounds__(kScoreThreads, 4) void q8_score_kernel(SelectArgs a) {
