@@ -533,7 +533,8 @@ typedef struct {
  * Writes the page-table entries of the pages that are begun (no others), and everything else in rows.  min(T, T/P + 2B)
  * runs are always enough.  The inputs stay as they are: for the next step the caller copies kv_len to seq_len and counts[3] to
  * free_count.  The inputs must be other memory than rows' buffers, as some workgroups read them while others write those; kv_len as
- * seq_len or n_new and counts + 3 as free_count are refused (KVD_ERR_ARG).  If the step does not fit, counts[4] says why, and it has no rows, no runs and no new blocks (kv_len = seq_len).
+ * seq_len or n_new and counts + 3 as free_count are refused (KVD_ERR_ARG).  If the step does not fit, counts[4] says why, and it has
+ * no rows, no runs and no new blocks (kv_len = seq_len).
  * A last page that is partly filled is continued in place: it must not be shared with another sequence. */
 int kvd_q8_map(const kvd_q8_rows* rows, const int32_t* seq_len, const int32_t* n_new, const int32_t* free_blocks,
                int32_t n_free, const int32_t* free_count, void* stream);
@@ -570,8 +571,8 @@ int kvd_q8_select(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void
  *   q [T][Hq][D] kv_dtype, rows q_stride elements apart;  out [T][Hq][D] kv_dtype;  lse [T][Hq] fp32 or NULL.
  * out = softmax(scale * q K^T) V, lse = log sum exp of the scaled logits; 0 and -infinity where a row sees nothing.  Sums,
  * maxima and accumulators are fp32; the weights that multiply V have 16 bits (off by 2^-16 of themselves at most), but 8 (2^-8)
- * where kv_dtype is bf16, sel_pages NULL and ceil(T / B) * G > 32.  No value is an infinity on the way, 448 * 2^120 neither; a
- * logit of what a row sees has to be finite in fp32.  Rows without a sequence are left as they were.  kv_len and row_start must be those of
+ * where kv_dtype is bf16, sel_pages NULL and ceil(T / B) * G > 32.  No value is an infinity on the way, 448 * 2^120 neither; the
+ * products q K^T of what a row sees, and its logits, have to be finite in fp32.  Rows without a sequence are left as they were.  kv_len and row_start must be those of
  * row_seq and row_pos. */
 int kvd_q8_attn(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, const int32_t* sel_pages,
                 int32_t topk_pages, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);

@@ -19,8 +19,8 @@
 // all their bits where values were 2^30 apart.)  The weights' bits: DUP (one row of up to 8 heads): the 16 columns hold each head
 // twice, and the second copy takes what rounding P to bf16 left of it: P is then 16 bits long at the price of nothing, as the
 // columns would be empty.  TWO: a product more for that rest, which costs 2 % where a few rows wait for the memory.  Many rows of bf16
-// do without it: P is rounded to bf16 there, by 2^-8 of each weight at most, like their output (530 us for 670 with it at 2 x 2048 rows of 32/8
-// heads behind 6144 tokens; f16, whose outputs show it, 698).
+// do without it: P is rounded to bf16 there, by 2^-8 of each weight at most, like their output (530 us for 670 with it at 2 x 2048
+// rows of 32/8 heads behind 6144 tokens; f16, whose outputs would show it, has it: 700).
 #include "kvd_q8.h"
 
 namespace kvd {
