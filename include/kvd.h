@@ -572,8 +572,8 @@ int kvd_q8_select(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void
  * out = softmax(scale * q K^T) V, lse = log sum exp of the scaled logits; 0 and -infinity where a row sees nothing.  Sums,
  * maxima and accumulators are fp32; the weights that multiply V have 16 bits (off by 2^-16 of themselves at most), but 8 (2^-8)
  * where kv_dtype is bf16, sel_pages NULL and ceil(T / B) * G > 32.  No value is an infinity on the way, 448 * 2^120 neither; the
- * products q K^T of what a row sees, and its logits, have to be finite in fp32.  Rows without a sequence are left as they were.  kv_len and row_start must be those of
- * row_seq and row_pos. */
+ * products q K^T of what a row sees, and its logits, have to be finite in fp32.  Rows without a sequence are left as they were.
+ * kv_len and row_start must be those of row_seq and row_pos. */
 int kvd_q8_attn(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, const int32_t* sel_pages,
                 int32_t topk_pages, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
