@@ -577,6 +577,99 @@ int kvd_q8_select(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void
 int kvd_q8_attn(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, const int32_t* sel_pages,
                 int32_t topk_pages, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- norm and rotation ------------------------------------------------------------------------ */
+/*
+ * What a step does with its query and key heads before kvd_q8_append, kvd_q4_append and attention: each head is normed, then its
+ * first rot_dim elements are turned in pairs by the row's position, and rounded once.
+ *   norm (with a weight w): y = x / sqrt(sum x^2 / D + eps) * w;  without: y = x
+ *   pair i = elements (i, i + rot_dim/2), or (2i, 2i + 1) if interleaved:  (a, b) -> (a cos t - b sin t, a sin t + b cos t),
+ *   t = pos[axis][row] * inv_freq[i], exact to 2^-24 of a turn for positions of any size (products of up to 2^29 turns)
+ * The pairs are dealt to the axes in order: the first axis_pairs[0] turn by axis 0 and so on (time, height and width of an image's
+ * patches; one axis for text).  The sum of squares has to be finite in fp32.
+ */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads;   /* 1..65536 each */
+  int32_t head_dim;                /* 128 */
+  int32_t kv_dtype;                /* kvd_dtype: type of q, k and the weights */
+  int32_t rot_dim;                 /* a multiple of 16, 0..128 */
+  int32_t interleaved;
+  int32_t n_axes;                  /* 1..4 */
+  int32_t axis_pairs[4];           /* the first n_axes add up to rot_dim / 2 */
+  float eps;
+  const void* q_weight;            /* dev [D] kv_dtype, 16-byte aligned, or NULL: no norm */
+  const void* k_weight;
+  const float* inv_freq;           /* dev [rot_dim / 2] */
+} kvd_rotary;
+
+/* Norms and turns q [T][Hq][D] into q_out and k [T][Hkv][D] into k_out: rows are the strides apart (elements, at least a row long,
+ * multiples of 8), heads D; q or k may be NULL (and its output with it).  In place (q_out == q with the same stride) is fine; apart
+ * from that the buffers must not overlap.
+ *   pos dev [n_axes][pos_stride] int32: a step's kvd_q8_rows.row_pos, for one axis.  Rows with a negative position on axis 0 are left as
+ * they were, as row_pos has them behind the last row.  n_rows <= 2^24.  q, k and their outputs start on 16 bytes. */
+int kvd_norm_rotate(const kvd_rotary* rotary, const int32_t* pos, int64_t pos_stride, int32_t n_rows, const void* q,
+                    int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out,
+                    int64_t k_out_stride, void* stream);
+
+/* ---- paged cache in 4 bits -------------------------------------------------------------------- */
+/*
+ * The same for contexts that do not fit in 8 bits either: 4.25 bits an element.  Page tables, rows and runs are those of the 8-bit
+ * cache (kvd_q8_map), and so are the sizes, the rules for buffers and workspaces, graphs, and bad input on the device.
+ *
+ * Values.  32 elements of a token and head (d/32 alike) share a scale 2^e, e in -96..125, stored as the byte e + 127; a code of type
+ * e2m1 (a sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6) stands for itself times that.  No two tokens share a scale: what is written stays as it is.
+ *
+ * Layout.  pages: [NB][Hkv][P/16] tiles of 16 tokens, 2176 bytes each, in the order in which a wave's lanes take them into matrix
+ * operands.  Token t, element d of a tile; of two codes of a byte the first has the lower bits:
+ *   key:   byte t*64 + d/2, code d%2;                       its scale: byte 2048 + (d/32)*16 + (t%4)*4 + t/4
+ *   value: byte 1024 + (d/32)*256 + (d%16)*16 + (d/16%2)*8 + t/2, code t%2;   its scale: byte 2112 + (d/32)*16 + t
+ * The pool starts on 128 bytes, and has less than 2^32 lines of 128 bytes.
+ */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads;
+  int32_t head_dim;        /* 128 */
+  int32_t page_size;       /* P */
+  int32_t n_blocks;        /* NB */
+  int32_t kv_dtype;        /* kvd_dtype: type of q, k, v and out */
+  float softmax_scale;     /* 0 means 1/sqrt(D) */
+  void* pages;             /* [NB][Hkv][P/16][2176] bytes */
+} kvd_q4_cache;
+
+/* What becomes of a row's scores.  A struct of zeros (or NULL in its place) changes nothing. */
+typedef struct {
+  float softcap;               /* > 0: logits x become softcap * tanh(x / softcap) */
+  int32_t window;              /* > 0: a row at position p sees tokens from p - window + 1 on */
+  const float* slopes;         /* dev [Hq] or NULL: slope * |p - t| is taken off the logit of token t (after the cap) */
+  const int32_t* row_from;     /* dev [T] or NULL: first position that a row sees (its document's first token) */
+  const int32_t* prefix_len;   /* dev [B] or NULL: every row of the sequence sees its first prefix_len tokens, later ones than itself too */
+} kvd_q4_scores;
+
+/* Quantises the step's keys and values into their pages, run by run and head by head; arguments as for kvd_q8_append.
+ * With amax the largest finite magnitude of 32 elements, e = the least >= -96 with amax <= 7 * 2^e, at most 125; codes are
+ * x / 2^e rounded to nearest, ties to the even code, and 6 for all that is larger.  An infinity becomes 6 * 2^e with its sign, a NaN
+ * becomes 0.  A run that begins its page sets the codes behind it to 0 and their scales to 2^-96; nothing else of a page changes. */
+int kvd_q4_append(const kvd_q4_cache* cache, const kvd_q8_rows* rows, const void* k_new, int64_t k_stride,
+                  const void* v_new, int64_t v_stride, void* stream);
+
+/* Reads the rows' tokens back: k, v [T][Hkv][D] kv_dtype, rows the strides apart (elements, at least a row long, multiples of 8).
+ * Uses page_table, row_seq and row_pos, in any order and as often as wanted: a caller that wants a whole context names its positions.
+ * Exact, but for magnitudes beyond f16's largest, which become that.  Rows without a token or block are left as they were. */
+int kvd_q4_read(const kvd_q4_cache* cache, const kvd_q8_rows* rows, void* k, int64_t k_stride, void* v, int64_t v_stride,
+                void* stream);
+
+/* Bytes of workspace that kvd_q4_attn needs for these sizes, or a negative kvd_status; to be used like that of kvd_q8_attn. */
+int64_t kvd_q4_workspace_bytes(const kvd_q4_cache* cache, const kvd_q8_rows* rows);
+
+/* Attention of every row over the tokens that it sees: those from max(row_from, p - window + 1, 0) to max(p, min(prefix_len, kv_len) - 1),
+ * p its position.
+ *   q [T][Hq][D] kv_dtype, rows q_stride elements apart;  out [T][Hq][D] kv_dtype;  lse [T][Hq] fp32 or NULL.
+ * out = softmax(f(scale * q K^T)) V, lse = log sum exp of the logits; 0 and -infinity where a row sees nothing.  Sums, maxima and
+ * accumulators are fp32.  Queries are exact to 2^-22 of the row's and head's largest element (f16: 2^-26); weights that multiply V
+ * are off by 2^-8 of themselves at most where kv_dtype is bf16 (f16: 2^-12), or by 2^-22 (2^-26) of the largest weight times scale among 128
+ * tokens, whichever is more.  The products q K^T of what a row sees, and its logits, have to be finite in fp32; a row and head with a query that is
+ * not finite gives NaN.  Rows without a sequence are left as they were.  kv_len and row_start must be those of row_seq and row_pos. */
+int kvd_q4_attn(const kvd_q4_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, const kvd_q4_scores* scores,
+                void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* ---- counters ------------------------------------------------------------------------------ */
 
 /* mode 0: off.

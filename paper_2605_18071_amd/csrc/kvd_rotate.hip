@@ -1,0 +1,176 @@
+// Norm and rotation of a step's query and key heads in one pass: y = x / sqrt(mean x^2 + eps) * w, then pairs of elements turned
+// by their position's angle, rounded once.  Angles are revolutions in fp64, position * frequency / 2 pi, of which the fraction
+// is kept: a position beyond 2^20 still has its angle to 2^-26 of a turn.  Bound by the memory (2 bytes an element read and
+// 2 written); sines are the work of one thread for each pair and row, and shared by the row's heads through LDS.
+#include "kvd_q8.h"
+
+namespace kvd {
+namespace q8 {
+
+constexpr int kRotThreads = 256;
+constexpr int kMaxPairs = kHeadDim / 2;
+constexpr int kMaxRotRows = 1 << 24;
+constexpr int kMaxRotHeads = 65536;
+
+struct RotateArgs {
+  const uint16_t *q, *k, *q_weight, *k_weight;
+  uint16_t *q_out, *k_out;
+  long long q_stride, k_stride, q_out_stride, k_out_stride, pos_stride;
+  const int32_t* pos;
+  const float* inv_freq;
+  int T, Hq, Hk, pairs, axis_end[4];           // axis_end: first pair behind the axis
+  float eps;
+};
+
+// NR rows a workgroup; 16 lanes have a head, 8 elements each.  NEAR: a pair's elements are neighbours, else `pairs` apart.
+template <bool BF16, bool NEAR, int NR>
+__global__ __launch_bounds__(kRotThreads) void norm_rotate_kernel(RotateArgs a) {
+  constexpr int kGroups = kRotThreads / 16;    // heads at a time
+  __shared__ float2 turn[NR][kMaxPairs];
+  const int tid = threadIdx.x, j = tid & 15, group = tid >> 4;
+  const long long row0 = (long long)blockIdx.x * NR;
+  const long long row = row0 + group % NR;
+  const int heads = a.Hq + a.Hk, per = kGroups / NR * gridDim.y;
+  int head = blockIdx.y * (kGroups / NR) + group / NR;
+  const bool real = row < a.T && a.pos[row] >= 0;
+  auto at = [&](int h) {
+    return h < a.Hq ? a.q + row * a.q_stride + (long long)h * kHeadDim + j * 8
+                    : a.k + row * a.k_stride + (long long)(h - a.Hq) * kHeadDim + j * 8;
+  };
+  uint4 x = make_uint4(0, 0, 0, 0);
+  if (real && head < heads) x = *reinterpret_cast<const uint4*>(at(head));
+  for (int i = tid; i < NR * kMaxPairs; i += kRotThreads) {
+    const int r = i / kMaxPairs, p = i % kMaxPairs;
+    if (p < a.pairs && row0 + r < a.T) {
+      const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
+      const double turns = (double)a.pos[axis * a.pos_stride + row0 + r] * ((double)a.inv_freq[p] * 0.15915494309189533577);
+      float s, c;
+      sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+      turn[r][p] = make_float2(c, s);
+    }
+  }
+  __syncthreads();
+  // the lane's cosines and sines: of its four pairs, or of the eight that its elements are one half of
+  const int half = a.pairs / 8;                // lanes of the first elements of pairs that lie apart
+  const bool turned = NEAR ? j < 2 * half : j < 2 * half, second = !NEAR && j >= half;
+  float2 t[NEAR ? 4 : 8];
+  if (turned)
+#pragma unroll
+    for (int i = 0; i < (NEAR ? 4 : 8); ++i) t[i] = turn[group % NR][NEAR ? j * 4 + i : (second ? j - half : j) * 8 + i];
+  const int lane = tid % kWave, partner = (lane & ~15) + (turned ? (second ? j - half : j + half) : j);
+  // weights: of the lane's elements and of its partner's, of both kinds of heads
+  uint4 wq = make_uint4(0, 0, 0, 0), wk = wq, vq = wq, vk = wq;
+  if (a.q_weight) {
+    wq = *reinterpret_cast<const uint4*>(a.q_weight + j * 8);
+    vq = *reinterpret_cast<const uint4*>(a.q_weight + (partner & 15) * 8);
+  }
+  if (a.k_weight) {
+    wk = *reinterpret_cast<const uint4*>(a.k_weight + j * 8);
+    vk = *reinterpret_cast<const uint4*>(a.k_weight + (partner & 15) * 8);
+  }
+  if (!real) return;                           // (whole groups of 16 lanes)
+  for (; head < heads; head += per) {
+    const bool is_q = head < a.Hq, norm = (is_q ? a.q_weight : a.k_weight) != nullptr;
+    uint4 next = x;
+    if (head + per < heads) next = *reinterpret_cast<const uint4*>(at(head + per));
+    float f[8], g[8];
+    cvt8<BF16>(x, f);
+    if (!NEAR) {
+      const uint4 y = make_uint4(__shfl(x.x, partner, kWave), __shfl(x.y, partner, kWave), __shfl(x.z, partner, kWave), __shfl(x.w, partner, kWave));
+      cvt8<BF16>(y, g);
+    }
+    if (norm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += f[i] * f[i];
+      const float inv = rsqrtf(row16_allreduce_sum(sum) * (1.f / kHeadDim) + a.eps);
+      const uint4 mine = is_q ? wq : wk, theirs = is_q ? vq : vk;
+      float w[8];
+      cvt8<BF16>(mine, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= inv * w[i];
+      if (!NEAR) {
+        cvt8<BF16>(theirs, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] *= inv * w[i];
+      }
+    }
+    if (turned) {
+      if constexpr (NEAR) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float u = f[2 * i], v = f[2 * i + 1];
+          f[2 * i] = u * t[i].x - v * t[i].y;
+          f[2 * i + 1] = u * t[i].y + v * t[i].x;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = second ? g[i] * t[i].y + f[i] * t[i].x : f[i] * t[i].x - g[i] * t[i].y;
+      }
+    }
+    uint16_t* to = is_q ? a.q_out + row * a.q_out_stride + (long long)head * kHeadDim + j * 8
+                        : a.k_out + row * a.k_out_stride + (long long)(head - a.Hq) * kHeadDim + j * 8;
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack2<BF16>(f[0], f[1]), pack2<BF16>(f[2], f[3]), pack2<BF16>(f[4], f[5]), pack2<BF16>(f[6], f[7]));
+    x = next;
+  }
+}
+
+template <bool BF16, bool NEAR>
+static void launch_rotate(const RotateArgs& a, hipStream_t s) {
+  // few rows are spread over the CUs, a row each and its heads over several workgroups; many share the workgroups' beginning
+  if (a.T >= 2048) hipLaunchKernelGGL((norm_rotate_kernel<BF16, NEAR, 4>), dim3((a.T + 3) / 4), dim3(kRotThreads), 0, s, a);
+  else hipLaunchKernelGGL((norm_rotate_kernel<BF16, NEAR, 1>), dim3(a.T, a.T <= 256 && a.Hq + a.Hk > 16 ? 2 : 1), dim3(kRotThreads), 0, s, a);
+}
+
+}  // namespace q8
+}  // namespace kvd
+
+extern "C" int kvd_norm_rotate(const kvd_rotary* c, const int32_t* pos, int64_t pos_stride, int32_t n_rows, const void* q,
+                               int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out,
+                               int64_t k_out_stride, void* stream) {
+  using namespace kvd::q8;
+  if (!c) return KVD_ERR_ARG;
+  if (c->kv_dtype != KVD_F16 && c->kv_dtype != KVD_BF16) return KVD_ERR_DTYPE;
+  if (c->head_dim != kvd::kHeadDim || n_rows < 1 || n_rows > kMaxRotRows) return KVD_ERR_SHAPE;
+  if (c->rot_dim < 0 || c->rot_dim > kvd::kHeadDim || c->rot_dim % 16 || c->n_axes < 1 || c->n_axes > 4) return KVD_ERR_SHAPE;
+  RotateArgs a = {};
+  a.pairs = c->rot_dim / 2;
+  int end = 0;
+  for (int i = 0; i < 4; ++i) {
+    if (i < c->n_axes) {
+      if (c->axis_pairs[i] < 0 || c->axis_pairs[i] > a.pairs - end) return KVD_ERR_SHAPE;
+      end += c->axis_pairs[i];
+    }
+    a.axis_end[i] = i < c->n_axes - 1 ? end : a.pairs;
+  }
+  if (end != a.pairs) return KVD_ERR_SHAPE;
+  if (pos_stride < n_rows && c->n_axes > 1) return KVD_ERR_SHAPE;
+  if (!(c->eps >= 0.f) || isinf(c->eps)) return KVD_ERR_ARG;
+  if (!aligned(pos, 4) || (a.pairs > 0 && !aligned(c->inv_freq, 4)) || (!q && !k)) return KVD_ERR_ARG;
+  auto tensor = [](const void* x, int64_t stride, void* out, int64_t out_stride, int heads, const void* weight) -> int {
+    if (heads < 1 || heads > kMaxRotHeads || !stride_ok(stride, heads) || !stride_ok(out_stride, heads)) return KVD_ERR_SHAPE;
+    if (!aligned(x, 16) || !aligned(out, 16) || (weight && !aligned(weight, 16))) return KVD_ERR_ARG;
+    return x == out && stride != out_stride ? KVD_ERR_ARG : KVD_OK;
+  };
+  if (q) {
+    if (int e = tensor(q, q_stride, q_out, q_out_stride, c->n_q_heads, c->q_weight)) return e;
+    a.Hq = c->n_q_heads;
+  }
+  if (k) {
+    if (int e = tensor(k, k_stride, k_out, k_out_stride, c->n_kv_heads, c->k_weight)) return e;
+    a.Hk = c->n_kv_heads;
+  }
+  a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k);
+  a.q_weight = static_cast<const uint16_t*>(c->q_weight); a.k_weight = static_cast<const uint16_t*>(c->k_weight);
+  a.q_out = static_cast<uint16_t*>(q_out); a.k_out = static_cast<uint16_t*>(k_out);
+  a.q_stride = q_stride; a.k_stride = k_stride; a.q_out_stride = q_out_stride; a.k_out_stride = k_out_stride;
+  a.pos_stride = pos_stride; a.pos = pos; a.inv_freq = c->inv_freq;
+  a.T = n_rows; a.eps = c->eps;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (c->kv_dtype == KVD_BF16) {
+    if (c->interleaved) launch_rotate<true, true>(a, s); else launch_rotate<true, false>(a, s);
+  } else {
+    if (c->interleaved) launch_rotate<false, true>(a, s); else launch_rotate<false, false>(a, s);
+  }
+  return launched();
+}

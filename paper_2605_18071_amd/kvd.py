@@ -77,6 +77,27 @@ class KvdQ8Rows(C.Structure):
     ]
 
 
+class KvdRotary(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("kv_dtype", C.c_int32),
+        ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("axis_pairs", C.c_int32 * 4),
+        ("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p),
+    ]
+
+
+class KvdQ4Cache(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+        ("n_blocks", C.c_int32), ("kv_dtype", C.c_int32), ("softmax_scale", C.c_float), ("pages", C.c_void_p),
+    ]
+
+
+class KvdQ4Scores(C.Structure):
+    _fields_ = [
+        ("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("row_from", C.c_void_p), ("prefix_len", C.c_void_p),
+    ]
+
+
 EXPORTS = [
     "kvd_create", "kvd_destroy", "kvd_strerror", "kvd_last_hip_error", "kvd_abi_version",
     "kvd_bind_summaries", "kvd_bind_host_store", "kvd_bind_slot_pool", "kvd_set_seq_lens",
@@ -89,6 +110,7 @@ EXPORTS = [
     "kvd_step_tiered", "kvd_step_layers", "kvd_sparse_decode_attn_noalloc",
     "kvd_set_step_shape", "kvd_get_step_shape", "kvd_calibrate_step_shape",
     "kvd_q8_map", "kvd_q8_append", "kvd_q8_workspace_bytes", "kvd_q8_select", "kvd_q8_attn",
+    "kvd_norm_rotate", "kvd_q4_append", "kvd_q4_read", "kvd_q4_workspace_bytes", "kvd_q4_attn",
 ]
 
 _lib = None
@@ -160,6 +182,11 @@ def load() -> C.CDLL:
         "kvd_q8_workspace_bytes": [vp, vp, i32],
         "kvd_q8_select": [vp, vp, vp, C.c_int64, vp, i32, vp, C.c_int64, vp],
         "kvd_q8_attn": [vp, vp, vp, C.c_int64, vp, i32, vp, vp, vp, C.c_int64, vp],
+        "kvd_norm_rotate": [vp, vp, C.c_int64, i32] + [vp, C.c_int64] * 4 + [vp],
+        "kvd_q4_append": [vp, vp, vp, C.c_int64, vp, C.c_int64, vp],
+        "kvd_q4_read": [vp, vp, vp, C.c_int64, vp, C.c_int64, vp],
+        "kvd_q4_workspace_bytes": [vp, vp],
+        "kvd_q4_attn": [vp, vp, vp, C.c_int64, vp, vp, vp, vp, C.c_int64, vp],
         "kvd_sparse_decode_attn_noalloc": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, C.c_float, i32, vp],
     }
     for name, args in protos.items():
@@ -167,6 +194,7 @@ def load() -> C.CDLL:
         fn.argtypes = args
         fn.restype = C.c_int
     lib.kvd_q8_workspace_bytes.restype = C.c_int64
+    lib.kvd_q4_workspace_bytes.restype = C.c_int64
     lib.kvd_strerror.argtypes = [C.c_int]
     lib.kvd_strerror.restype = C.c_char_p
     _lib = lib
@@ -601,7 +629,32 @@ class Q8Rows(_OnDevice):
                    free_blocks.numel(), free_count.data_ptr())
 
 
-class Q8Cache(_OnDevice):
+class _Heads(_OnDevice):
+    """What has tensors of [rows][heads][head_dim]."""
+
+    def _rowed(self, name: str, t: torch.Tensor, heads: int, n_rows: int) -> int:
+        """Stride of a [rows][heads][head_dim] tensor whose rows may lie apart."""
+        D = self.head_dim
+        row, head, element = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if t.shape != (n_rows, heads, D) or t.dtype is not self.kv_dtype or t.device != self.device or head != D or element != 1:
+            raise ValueError(f"{name}: a {self.kv_dtype} tensor of {(n_rows, heads, D)} on {self.device} with whole rows is wanted, "
+                             f"got {t.dtype} of {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+        return row if n_rows > 1 else heads * D
+
+    def _check_rows(self, rows: Q8Rows, workspace: Optional[torch.Tensor] = None):
+        if rows.device != self.device:
+            raise ValueError("the rows and the cache are on different devices")
+        if workspace is not None and (workspace.device != self.device or not workspace.is_contiguous()):
+            raise ValueError("workspace: a contiguous tensor on the cache's device is wanted")
+
+
+def _kv_type(kv_dtype) -> torch.dtype:
+    kv_dtype = {KVD_F16: torch.float16, KVD_BF16: torch.bfloat16}.get(kv_dtype, kv_dtype)
+    _need(kv_dtype in (torch.float16, torch.bfloat16), "kv_dtype: float16 or bfloat16 is wanted")
+    return kv_dtype
+
+
+class Q8Cache(_Heads):
     """One kvd_q8_cache: the 8-bit pages of a layer, over `buffers` (a dict of pages, exps, means and mean_scales) where
     given, otherwise over new ones."""
 
@@ -612,8 +665,7 @@ class Q8Cache(_OnDevice):
         _need(not set(buffers) - {"pages", "exps", "means", "mean_scales"}, "buffers: pages, exps, means and mean_scales are wanted")
         self.device = next(iter(buffers.values())).device if buffers else _cuda(device)
         _need(page_size >= 16 and page_size % 16 == 0, "page_size: a multiple of 16 is wanted")
-        self.kv_dtype = {KVD_F16: torch.float16, KVD_BF16: torch.bfloat16}.get(kv_dtype, kv_dtype)
-        _need(self.kv_dtype in (torch.float16, torch.bfloat16), "kv_dtype: float16 or bfloat16 is wanted")
+        self.kv_dtype = _kv_type(kv_dtype)
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         shapes = dict(pages=((n_blocks, n_kv_heads, page_size // 16, 2, 2048), torch.uint8),
                       exps=((n_blocks, n_kv_heads, 2), torch.int8), means=((n_blocks, n_kv_heads, head_dim), torch.int8),
@@ -633,21 +685,6 @@ class Q8Cache(_OnDevice):
         if n < 0:
             raise KvdError(int(n), "kvd_q8_workspace_bytes")
         return torch.zeros((n + 15) // 16 * 4, dtype=torch.int32, device=self.device)
-
-    def _rowed(self, name: str, t: torch.Tensor, heads: int, n_rows: int) -> int:
-        """Stride of a [rows][heads][head_dim] tensor whose rows may lie apart."""
-        D = self.head_dim
-        row, head, element = t.stride() if t.dim() == 3 else (0, 0, 0)
-        if t.shape != (n_rows, heads, D) or t.dtype is not self.kv_dtype or t.device != self.device or head != D or element != 1:
-            raise ValueError(f"{name}: a {self.kv_dtype} tensor of {(n_rows, heads, D)} on {self.device} with whole rows is wanted, "
-                             f"got {t.dtype} of {tuple(t.shape)}, strides {t.stride()} on {t.device}")
-        return row if n_rows > 1 else heads * D
-
-    def _check_rows(self, rows: Q8Rows, workspace: Optional[torch.Tensor] = None):
-        if rows.device != self.device:
-            raise ValueError("the rows and the cache are on different devices")
-        if workspace is not None and (workspace.device != self.device or not workspace.is_contiguous()):
-            raise ValueError("workspace: a contiguous tensor on the cache's device is wanted")
 
     def append(self, rows: Q8Rows, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
         """kvd_q8_append: the rows' keys and values [rows][kv heads][head_dim] into their pages."""
@@ -678,4 +715,108 @@ class Q8Cache(_OnDevice):
             k = sel_pages.shape[-1]
             _buffer("sel_pages", sel_pages, (rows.n_rows, self.n_kv_heads, k), torch.int32, self.device)
         self._call("kvd_q8_attn", stream, self._ref, rows._ref, q.data_ptr(), qs, _ptr(sel_pages), k, out.data_ptr(), _ptr(lse),
+                   workspace.data_ptr(), workspace.nbytes)
+
+
+# ---- norm and rotation
+
+class Rotary(_Heads):
+    """One kvd_rotary: norm (where weights are given) and rotation by inv_freq (fp32, one for each pair of elements) of query and key
+    heads.  axis_pairs: the pairs that turn by each axis of the positions; all by one if it is not given."""
+
+    def __init__(self, inv_freq: torch.Tensor, *, n_q_heads: int, n_kv_heads: int, kv_dtype, head_dim: int = 128, interleaved: bool = False,
+                 axis_pairs: Optional[Sequence[int]] = None, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        self.lib = load()
+        self.device = inv_freq.device
+        self.kv_dtype = _kv_type(kv_dtype)
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
+        pairs = inv_freq.numel()
+        self.inv_freq = _buffer("inv_freq", inv_freq, (pairs,), torch.float32, self.device)
+        axis_pairs = [pairs] if axis_pairs is None else [int(n) for n in axis_pairs]
+        _need(1 <= len(axis_pairs) <= 4 and min(axis_pairs) >= 0 and sum(axis_pairs) == pairs,
+              "axis_pairs: one to four counts that add up to inv_freq's are wanted")
+        self.n_axes = len(axis_pairs)
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                _buffer(name, w, (head_dim,), self.kv_dtype, self.device)
+            setattr(self, name, w)
+        self.c = KvdRotary(n_q_heads, n_kv_heads, head_dim, KVD_F16 if self.kv_dtype == torch.float16 else KVD_BF16, 2 * pairs,
+                           1 if interleaved else 0, self.n_axes, (C.c_int32 * 4)(*axis_pairs), eps, _ptr(q_weight), _ptr(k_weight),
+                           self.inv_freq.data_ptr())
+        self._ref = C.byref(self.c)
+
+    def apply(self, positions: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, *,
+              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+        """kvd_norm_rotate: q [rows][q heads][head_dim] and k [rows][kv heads][head_dim] (either may be None) at positions [rows], as a step's
+        row_pos, or [axes][rows]; into q_out and k_out, or in place.  Rows with a negative position are left out."""
+        n_rows = positions.shape[-1]
+        shape = (n_rows,) if self.n_axes == 1 and positions.dim() == 1 else (self.n_axes, n_rows)
+        _buffer("positions", positions, shape, torch.int32, self.device)
+        _need(q is not None or k is not None, "q or k is wanted")
+        args = []
+        for name, x, out, heads in (("q", q, q_out, self.n_q_heads), ("k", k, k_out, self.n_kv_heads)):
+            _need(x is not None or out is None, f"{name}_out: there is no {name}")
+            out = x if out is None else out
+            args += [_ptr(x), 0 if x is None else self._rowed(name, x, heads, n_rows),
+                     _ptr(out), 0 if out is None else self._rowed(name + "_out", out, heads, n_rows)]
+        self._call("kvd_norm_rotate", stream, self._ref, positions.data_ptr(), n_rows, n_rows, *args)
+
+
+# ---- paged cache in 4 bits
+
+class Q4Cache(_Heads):
+    """One kvd_q4_cache: the 4-bit pages of a layer, over `pages` (uint8 [blocks][kv heads][page_size / 16][2176]) where given,
+    otherwise over new ones.  Its rows are Q8Rows, and one Q8Rows may serve caches of both kinds."""
+
+    def __init__(self, *, n_blocks: int, n_q_heads: int, n_kv_heads: int, page_size: int, kv_dtype, head_dim: int = 128,
+                 softmax_scale: float = 0.0, device="cuda", pages: Optional[torch.Tensor] = None):
+        self.lib = load()
+        self.device = pages.device if pages is not None else _cuda(device)
+        _need(page_size >= 16 and page_size % 16 == 0, "page_size: a multiple of 16 is wanted")
+        self.kv_dtype = _kv_type(kv_dtype)
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
+        shape = (n_blocks, n_kv_heads, page_size // 16, 2176)
+        self.pages = torch.zeros(shape, dtype=torch.uint8, device=self.device) if pages is None else _buffer("pages", pages, shape, torch.uint8,
+                                                                                                             self.device)
+        self.c = KvdQ4Cache(n_q_heads, n_kv_heads, head_dim, page_size, n_blocks,
+                            KVD_F16 if self.kv_dtype == torch.float16 else KVD_BF16, softmax_scale, self.pages.data_ptr())
+        self._ref = C.byref(self.c)
+
+    def workspace(self, rows: Q8Rows) -> torch.Tensor:
+        """A new workspace for attend of these rows.  Calls that overlap in time need one each."""
+        n = self.lib.kvd_q4_workspace_bytes(self._ref, rows._ref)
+        if n < 0:
+            raise KvdError(int(n), "kvd_q4_workspace_bytes")
+        return torch.zeros((n + 15) // 16 * 4, dtype=torch.int32, device=self.device)
+
+    def append(self, rows: Q8Rows, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
+        """kvd_q4_append: the rows' keys and values [rows][kv heads][head_dim] into their pages."""
+        self._check_rows(rows)
+        ks = self._rowed("k_new", k_new, self.n_kv_heads, rows.n_rows)
+        vs = self._rowed("v_new", v_new, self.n_kv_heads, rows.n_rows)
+        self._call("kvd_q4_append", stream, self._ref, rows._ref, k_new.data_ptr(), ks, v_new.data_ptr(), vs)
+
+    def read(self, rows: Q8Rows, k: torch.Tensor, v: torch.Tensor, stream=None):
+        """kvd_q4_read: the keys and values of the rows' tokens into k and v [rows][kv heads][head_dim]."""
+        self._check_rows(rows)
+        ks = self._rowed("k", k, self.n_kv_heads, rows.n_rows)
+        vs = self._rowed("v", v, self.n_kv_heads, rows.n_rows)
+        self._call("kvd_q4_read", stream, self._ref, rows._ref, k.data_ptr(), ks, v.data_ptr(), vs)
+
+    def attend(self, rows: Q8Rows, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, *,
+               softcap: float = 0.0, window: int = 0, slopes: Optional[torch.Tensor] = None, row_from: Optional[torch.Tensor] = None,
+               prefix_len: Optional[torch.Tensor] = None, stream=None):
+        """kvd_q4_attn: attention of the rows over what they see of their sequences."""
+        self._check_rows(rows, workspace)
+        qs = self._rowed("q", q, self.n_q_heads, rows.n_rows)
+        _buffer("out", out, (rows.n_rows, self.n_q_heads, self.head_dim), self.kv_dtype, self.device)
+        if lse is not None:
+            _buffer("lse", lse, (rows.n_rows, self.n_q_heads), torch.float32, self.device)
+        for name, t, n, dtype in (("slopes", slopes, self.n_q_heads, torch.float32), ("row_from", row_from, rows.n_rows, torch.int32),
+                                  ("prefix_len", prefix_len, rows.n_seqs, torch.int32)):
+            if t is not None:
+                _buffer(name, t, (n,), dtype, self.device)
+        scores = KvdQ4Scores(softcap, window, _ptr(slopes), _ptr(row_from), _ptr(prefix_len))
+        self._call("kvd_q4_attn", stream, self._ref, rows._ref, q.data_ptr(), qs, C.byref(scores), out.data_ptr(), _ptr(lse),
                    workspace.data_ptr(), workspace.nbytes)
