@@ -13,8 +13,6 @@ using q8::stride_ok;
 using q8::two_to;
 typedef q8::f32x2 f32x2;
 typedef q8::f32x4 f32x4;
-typedef short i16x2 __attribute__((ext_vector_type(2)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 32;                     // elements of a scale
 constexpr int kValues = 1024, kKeyScales = 2048, kValueScales = 2112;    // where they begin in a tile

@@ -1,21 +1,21 @@
 // Attention of a step's rows over the pages of the 4-bit cache.
 //
-// S^T = K Q^T and O^T += V^T P^T on the matrix cores' scaled products of 128 elements: codes go into them as they lie in memory,
-// with no widening, and a wave takes 128 tokens at a time.  A product has one operand in 4 bits (keys, values) and one in 8 (e4m3:
-// queries, weights).  16-bit numbers go into 8-bit operands in pieces of four bits each, the second piece what the first one
-// left, a sixteenth as large at most: two pieces hold a bf16, three an f16.  Keys' scales (one for 32 elements of a token) are
-// the first product's own; values' scales are one for 32 elements of a token too, which the second product sums over, so that
-// they go into the weights: each group of 32 columns of V has weights of its own, p * 2^e.
+// S^T = K Q^T and O^T += V^T P^T on the matrix cores, 128 tokens a wave and step: a result's columns are query rows (a row of the
+// step and a head of the group), and the softmaxed S^T of a lane is its operand of the second product, element for element,
+// because of the order in which tokens are dealt to the first product's rows.  Codes come from memory in operand order, 16 bytes a lane,
+// and become bf16 in registers, which holds every one of them times its scale.  Keys take their scales there.  Values' scales are one
+// for 32 elements of a token, which the second product sums over: they go into the weights, so that each group of 32 columns of V has
+// weights of its own, p * 2^e.  Where columns would be empty they repeat the rows (REP): each copy weighs the values of a fraction of
+// the groups.
 //
-// A result's columns are query rows (a row of the step and a head of the group) and the softmaxed S^T of a lane is its operand
-// of the second product, element for element, because of the order in which tokens are dealt to the first product's rows.
-// Where columns would be empty they repeat the rows (REP): each copy weighs the values of a fraction of the groups.
+// (The matrix cores' own products of 4-bit operands with scales take keys and values as they are, but their sums of eight products
+// keep 13 bits below the largest: logits of 140 came out 2^-16 off, and small weights beside a large one got lost.)
 //
 // One pass with a running reference m and sum l of a column: p = 2^(x - m).  m is kHead above the largest logit when it is set, and
 // is raised only when a logit passes that by more than kSlack, so that the accumulators are rarely touched; p then stays below
-// 2^(kSlack - kHead).  Weights are 8 bits long for bf16 and 12 for f16 (off by 2^-8 and 2^-12 of themselves at most, like a
-// rounding of their type), and never off by less than 2^-22 and 2^-26 of the largest of 128 tokens' p * 2^e.
-// The accumulators are taken times 2^-kDown, so that weights below 2^-4 and values below 2^128 of 2^24 tokens stay finite.
+// 2^(kSlack - kHead).  Weights are taken times 2^-kDown, so that those below 2^-4 and values below 2^128 of 2^24 tokens stay finite.
+// bf16: they are rounded to bf16, by 2^-8 of themselves at most, like their output.  f16, whose outputs would show it: a
+// second product takes what the rounding left (2^-17), and the first one has the queries in two parts of bf16 too.
 #include "kvd_q4.h"
 #include "kvd_q8_deal.h"
 
@@ -24,6 +24,7 @@ namespace q4 {
 
 using q8::deal;
 using q8::Unit;
+using q8::bf16x8;
 
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnGroups = 512;               // workgroups: two for each CU
@@ -33,10 +34,10 @@ constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 // 8-byte words of a partial result: accumulators, then a maximum and a sum a column
 __host__ __device__ constexpr size_t part_words(int groups) { return (size_t)groups * (16 * kWave + 16); }
 constexpr float kLowest = -3.0e38f, kSlack = 8.f, kHead = 12.f;
-constexpr int kDown = 24, kLeastExp = -94;
+constexpr int kDown = 24;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr u32 kNoTile = 0xffffffffu;
-typedef int i32x4 __attribute__((ext_vector_type(4)));
+using q8::i32x4;
 
 __device__ __forceinline__ i32x4 load_codes(const unsigned char* p) { return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p)); }
 __device__ __forceinline__ i32x4 load_scales(const unsigned char* p) { return *reinterpret_cast<const i32x4*>(p); }
@@ -69,45 +70,38 @@ __device__ __forceinline__ float max_of_column(float x) {      // over the four 
   x = fmaxf(x, __shfl_xor(x, 16, kWave));
   return fmaxf(x, __shfl_xor(x, 32, kWave));
 }
-// The exponent E with top * 2^-E in [128, 256), where a piece's numbers lie best in e4m3
-__device__ __forceinline__ int exp_of(float top) { return max((int)(as_u32(top) >> 23) - 134, kLeastExp); }
-
-// 32 numbers times 2^-E to NP pieces of 8 bits, of which piece i stands for multiples of 2^(E - 4 i)
-template <int NP>
-__device__ __forceinline__ void pieces(float (&x)[32], int E, i32x8 (&to)[NP]) {
-#pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    const float scale = two_to(E - 4 * p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      i16x2 w = {0, 0};
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i], x[4 * i + 1], scale, false);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i + 2], x[4 * i + 3], scale, true);
-      to[p][i] = __builtin_bit_cast(int, w);
-      if (p + 1 < NP) {
-        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((u32)to[p][i], scale, false);
-        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((u32)to[p][i], scale, true);
-        x[4 * i] -= a[0]; x[4 * i + 1] -= a[1]; x[4 * i + 2] -= b[0]; x[4 * i + 3] -= b[1];
-      }
-    }
-  }
+__device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// Eight codes to an operand, times the scale
+__device__ __forceinline__ bf16x8 widen(int codes, float scale) {
+  const u32 w = (u32)codes;
+  const uint4 x = make_uint4(__builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                             __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                             __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                             __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
+  return __builtin_bit_cast(bf16x8, x);
 }
-// The scales' bytes of the pieces, piece i in byte i
-__device__ __forceinline__ int piece_scales(int E) {
-  const u32 b = (u32)(E + kBias);
-  return (int)(b | (b - 4) << 8 | (b - 8) << 16);
+// Eight numbers to NP operands: rounded to bf16, and what that left
+template <int NP>
+__device__ __forceinline__ void parts(const float* x, bf16x8 (&to)[NP]) {
+  u32 w[4], rest[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = pack2<true>(x[2 * i], x[2 * i + 1]);
+    if (NP > 1) rest[i] = pack2<true>(x[2 * i] - as_f32(w[i] << 16), x[2 * i + 1] - as_f32(w[i] & 0xffff0000u));
+  }
+  to[0] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+  if constexpr (NP > 1) to[1] = __builtin_bit_cast(bf16x8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
 }
 
 template <bool BF16, int NQ, int REP>
 struct Wave {
-  static constexpr int NP = BF16 ? 2 : 3;
+  static constexpr int NP = BF16 ? 1 : 2;      // parts of bf16 that a number of q's type has
   static constexpr int kCols = 16 / REP;       // columns that differ
   static constexpr int kGroups = 4 / REP;      // of V's groups of 32 columns, those that a lane weighs
   static_assert(NQ == 1 || REP == 1, "");
   f32x4 o[NQ][8];
   float m[NQ], l[NQ], slope[NQ];
-  i32x8 q[NQ][NP];
-  int qs[NQ];
+  bf16x8 q[NQ][4][NP];
   int lo[NQ], hi[NQ], pos[NQ];                 // first and last position that the lane's column sees, its own
   int lo_most, hi_least;                       // what every column sees lies between
   int t_first, t_behind;                       // tiles that any column sees
@@ -146,14 +140,13 @@ struct Wave {
       lo[g] = 0x7fffffff;
       hi[g] = -1;
       slope[g] = 0.f;
-      float x[32], top = 0.f;
       uint4 raw[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
       if (ok) {
-        const uint16_t* src = a.q + (long long)row * a.q_stride + (u.h * a.G + head) * kHeadDim + c * 16;
+        const uint16_t* src = a.q + (long long)row * a.q_stride + (u.h * a.G + head) * kHeadDim + c * 32;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const uint4*>(src + (i >> 1) * 64 + (i & 1) * 8);
+        for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const uint4*>(src + i * 8);
         lo[g] = a.window > 0 ? max(pos[g] - a.window + 1, 0) : 0;
         if (a.row_from) lo[g] = max(lo[g], a.row_from[row]);
         hi[g] = min(max(pos[g], prefix - 1), len - 1);
@@ -163,25 +156,20 @@ struct Wave {
         lo_most = max(lo_most, lo[g]);
         hi_least = min(hi_least, hi[g]);
       }
-      bool fine = true;
+      float off = 0.f;                         // a row with an infinity or a NaN gives NaN, and no other row does
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float f[8];
         cvt8<BF16>(raw[i], f);
 #pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          x[i * 8 + y] = f[y];
-          fine &= fabsf(f[y]) < INFINITY;
-          top = fmaxf(top, fabsf(f[y]));
-        }
+        for (int y = 0; y < 8; ++y) off += f[y] * 0.f;
+        parts<NP>(f, q[g][i]);
       }
-      top = max_of_column(fine ? top : INFINITY);
-      const int E = top < INFINITY ? exp_of(top) : 0;
-      if (!(top < INFINITY))                   // the row's result is a NaN, and no other's
+      off += __shfl_xor(off, 16, kWave);
+      off += __shfl_xor(off, 32, kWave);
+      if (off != 0.f)
 #pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] = NAN;
-      pieces<NP>(x, E, q[g]);
-      qs[g] = piece_scales(E);
+        for (int i = 0; i < 4; ++i) q[g][i][0] = __builtin_bit_cast(bf16x8, make_uint4(~0u, ~0u, ~0u, ~0u));
       m[g] = kLowest;
       l[g] = 0.f;
 #pragma unroll
@@ -230,44 +218,49 @@ struct Wave {
   __device__ __forceinline__ void load_keys(u32 lines) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const unsigned char* at = tile(lines, half * 4 + (n >> 2)) + (n & 3) * 64 + c * 16;
+      const unsigned char* at = tile(lines, 2 * (n >> 2) + half) + (n & 3) * 64 + c * 16;
 #pragma unroll
       for (int j = 0; j < 4; ++j) k[half * 4 + j] = load_codes(at + j * 256);
-      ks[half] = *reinterpret_cast<const u32*>(at - (n & 3) * 64 + kKeyScales + (n & 3) * 4);
+      ks[half] = *reinterpret_cast<const u32*>(at - (n & 3) * 60 + kKeyScales);
     }
   }
   __device__ __forceinline__ void load_values(u32 lines) {
-    const unsigned char *at0 = tile(lines, 2 * c) + kValues + n * 16, *at1 = tile(lines, 2 * c + 1) + kValues + n * 16;
+    const unsigned char *at0 = tile(lines, 2 * c), *at1 = tile(lines, 2 * c + 1);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      v[2 * x] = load_codes(at0 + x * 256);
-      v[2 * x + 1] = load_codes(at1 + x * 256);
+      v[2 * x] = load_codes(at0 + kValues + n * 16 + x * 256);
+      v[2 * x + 1] = load_codes(at1 + kValues + n * 16 + x * 256);
     }
-    const unsigned char *s0 = tile(lines, c) + kValueScales, *s1 = tile(lines, c + 4) + kValueScales;
 #pragma unroll
     for (int x = 0; x < kGroups; ++x) {
       const int group = x * REP + (REP > 1 ? n / kCols : 0);
-      vs[x][0] = load_scales(s0 + group * 16);
-      vs[x][1] = load_scales(s1 + group * 16);
+      vs[x][0] = load_scales(at0 + kValueScales + group * 16);
+      vs[x][1] = load_scales(at1 + kValueScales + group * 16);
     }
   }
 
   // ---- the step of tiles [t0, t0 + 8)
 
-  __device__ __forceinline__ void scores(int g, f32x4 (&s)[8]) {
+  // Row r of the products of tile j is token 32 (r / 4) + 4 j + r % 4 of the step, so that lane (c, n) gets tokens 32 c + 0..31 of column n
+  __device__ __forceinline__ void scores(f32x4 (&s)[NQ][8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    each_of<NP>([&](auto piece) {
-      each_of<8>([&](auto tile) {
-        constexpr int p = decltype(piece)::value, j = decltype(tile)::value;
-        const i32x8 A = __builtin_shufflevector(k[j], k[j], 0, 1, 2, 3, -1, -1, -1, -1);
-        s[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, q[g][p], s[j], 4, 0, j % 4, (int)ks[j / 4], p, qs[g]);
-      });
-    });
+    for (int j = 0; j < 8; ++j) {
+      const float scale = two_to((int)(ks[j / 4] >> (8 * (j % 4)) & 255) - kBias);
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) s[g][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bf16x8 A = widen(k[j][i], scale);
+#pragma unroll
+        for (int g = 0; g < NQ; ++g)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) s[g][j] = mfma32(A, q[g][i][p], s[g][j]);
+      }
+    }
   }
   // Products to logits in powers of two, -infinity where the column does not see the token
   __device__ __forceinline__ void logits(int g, int t0, f32x4 (&s)[8]) {
-    const int base = t0 * kTile, at = base + c * 16;
+    const int base = t0 * kTile, at = base + c * 32;
     if (a.cap_in != 0.f) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -284,15 +277,15 @@ struct Wave {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[j][i] -= slope[g] * fabsf((float)(pos[g] - (at + (j >> 2) * 64 + (j & 3) * 4 + i)));
+        for (int i = 0; i < 4; ++i) s[j][i] -= slope[g] * fabsf((float)(pos[g] - (at + j * 4 + i)));
     }
     if (base < lo_most || base + kStep * kTile - 1 > hi_least || __any(line == kNoTile)) {
-      const bool none[2] = {__shfl(line, c, kWave) == kNoTile, __shfl(line, c + 4, kWave) == kNoTile};
+      const bool none[2] = {__shfl(line, 2 * c, kWave) == kNoTile, __shfl(line, 2 * c + 1, kWave) == kNoTile};
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int t = at + (j >> 2) * 64 + (j & 3) * 4 + i;
+          const int t = at + j * 4 + i;
           if (none[j >> 2] || t < lo[g] || t > hi[g]) s[j][i] = -INFINITY;
         }
     }
@@ -320,29 +313,32 @@ struct Wave {
       }
     l[g] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
-  // The weights of a group of 32 columns of V, and what they add to it (REP > 1: to REP groups, of which one is this lane's)
+  // What the tokens add to 32 columns of V (REP > 1: to REP groups of them, of which one has this lane's weights)
   template <int X>
-  __device__ __forceinline__ void weigh(int g, const float (&p)[32]) {
-    float w[32], top = 0.f;
+  __device__ __forceinline__ void weigh(const float (&p)[NQ][32]) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const u32 word = vs[X][i >> 4][i >> 2 & 3];
-      w[i] = __builtin_amdgcn_ldexpf(p[i], (int)(word >> (8 * (i & 3)) & 255) - kBias);
+    for (int i = 0; i < 4; ++i) {              // eight of the lane's tokens
+      bf16x8 B[NQ][NP];
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) {
+        float w[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const u32 word = vs[X][i >> 1][(i & 1) * 2 + (y >> 2)];
+          w[y] = __builtin_amdgcn_ldexpf(p[g][8 * i + y], (int)(word >> (8 * (y & 3)) & 255) - (kBias + kDown));
+        }
+        parts<NP>(w, B[g]);
+      }
+#pragma unroll
+      for (int z = 0; z < 2 * REP; ++z) {
+        const int d = X * 2 * REP + z;         // 16 columns
+        const bf16x8 A = widen(v[d / 2 * 2 + (i >> 1)][d % 2 * 2 + (i & 1)], 1.f);
+#pragma unroll
+        for (int g = 0; g < NQ; ++g)
+#pragma unroll
+          for (int y = 0; y < NP; ++y) o[g][d] = mfma32(A, B[g][y], o[g][d]);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) top = max3(top, w[i], w[i + 1]);
-    const int E = exp_of(max_of_column(top));
-    i32x8 B[NP];
-    pieces<NP>(w, E, B);
-    const int bs = piece_scales(E - kDown);
-    each_of<2 * REP>([&](auto z) {
-      each_of<NP>([&](auto piece) {
-        constexpr int p = decltype(piece)::value, i = X * 2 * REP + decltype(z)::value;
-        const i32x8 A = i % 2 == 0 ? __builtin_shufflevector(v[i / 2 * 2], v[i / 2 * 2 + 1], 0, 1, 4, 5, -1, -1, -1, -1)
-                                   : __builtin_shufflevector(v[i / 2 * 2], v[i / 2 * 2 + 1], 2, 3, 6, 7, -1, -1, -1, -1);
-        o[g][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B[p], o[g][i], 4, 0, 0, kBias, p, bs);
-      });
-    });
   }
 
   // Tiles [from, to) of the unit.  Keys of the next step are asked for when those of this one have been taken, values likewise;
@@ -355,22 +351,22 @@ struct Wave {
       load_values(line);
       for (int t = from; t < to; t += kStep) {
         const bool more = t + kStep < to;
+        f32x4 s[NQ][8];
+        scores(s);
+        if (more) {
+          __builtin_amdgcn_sched_barrier(0);
+          line_next = line_of(t + kStep, block_next);
+          block_next = block_of(t + 2 * kStep, to);
+          load_keys(line_next);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        float p[NQ][32];
 #pragma unroll
         for (int g = 0; g < NQ; ++g) {
-          f32x4 s[8];
-          scores(g, s);
-          if (g == NQ - 1 && more) {
-            __builtin_amdgcn_sched_barrier(0);
-            line_next = line_of(t + kStep, block_next);
-            block_next = block_of(t + 2 * kStep, to);
-            load_keys(line_next);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          logits(g, t, s);
-          float p[32];
-          soften(g, s, p);
-          each_of<kGroups>([&](auto x) { weigh<decltype(x)::value>(g, p); });
+          logits(g, t, s[g]);
+          soften(g, s[g], p[g]);
         }
+        each_of<kGroups>([&](auto x) { weigh<decltype(x)::value>(p); });
         if (more) {
           __builtin_amdgcn_sched_barrier(0);
           line = line_next;
