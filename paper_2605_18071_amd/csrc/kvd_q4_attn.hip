@@ -1,20 +1,17 @@
 // Attention of a step's rows over the pages of the 4-bit cache.
 //
-// S^T = K Q^T and O^T += V^T P^T on the matrix cores, 128 tokens a wave and step: a result's columns are query rows (a row of the
-// step and a head of the group), and the softmaxed S^T of a lane is its operand of the second product, element for element,
-// because of the order in which tokens are dealt to the first product's rows.  Codes come from memory in operand order, 16 bytes a lane,
-// and become bf16 in registers, which holds every one of them times its scale.  Keys take their scales there.  Values' scales are one
-// for 32 elements of a token, which the second product sums over: they go into the weights, so that each group of 32 columns of V has
-// weights of its own, p * 2^e.  Where columns would be empty they repeat the rows (REP): each copy weighs the values of a fraction of
-// the groups.
+// S^T = K Q^T and O^T += V^T P^T on the matrix cores: a result's columns are query rows (a row of the step and a head of the group),
+// and the softmaxed S^T of a lane is its operand of the second product, element for element, because of the order in which
+// tokens are dealt to the first product's rows.  Codes come from memory in operand order, 16 bytes a lane, and become bf16 in
+// registers, which holds every one of them times its scale.
 //
 // (The matrix cores' own products of 4-bit operands with scales take keys and values as they are, but their sums of eight products
 // keep 13 bits below the largest: logits of 140 came out 2^-16 off, and small weights beside a large one got lost.)
 //
 // One pass with a running reference m and sum l of a column: p = 2^(x - m).  m is kHead above the largest logit when it is set, and
 // is raised only when a logit passes that by more than kSlack, so that the accumulators are rarely touched; p then stays below
-// 2^(kSlack - kHead).  Weights are taken times 2^-kDown, so that those below 2^-4 and values below 2^128 of 2^24 tokens stay finite.
-// bf16: they are rounded to bf16, by 2^-8 of themselves at most, like their output.  f16, whose outputs would show it: a
+// 2^(kSlack - kHead), so that 2^24 tokens' values of up to 2^128 have finite sums.
+// bf16: weights are rounded to bf16, by 2^-8 of themselves at most, like their output.  f16, whose outputs would show it: a
 // second product takes what the rounding left (2^-17), and the first one has the queries in two parts of bf16 too.
 #include "kvd_q4.h"
 #include "kvd_q8_deal.h"
@@ -22,25 +19,21 @@
 namespace kvd {
 namespace q4 {
 
-using q8::deal;
-using q8::Unit;
 using q8::bf16x8;
+using q8::deal;
+using q8::i32x4;
+using q8::Unit;
 
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnGroups = 512;               // workgroups: two for each CU
 constexpr int kStep = 8;                       // tiles that a wave takes at a time
 constexpr int kLeastTiles = 32;                // tiles of a workgroup at least
+constexpr int kPieceTiles = 64;                // tiles of a workgroup where there are few
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
-// 8-byte words of a partial result: accumulators, then a maximum and a sum a column
-__host__ __device__ constexpr size_t part_words(int groups) { return (size_t)groups * (16 * kWave + 16); }
-constexpr float kLowest = -3.0e38f, kSlack = 8.f, kHead = 12.f;
-constexpr int kDown = 24;
+constexpr int kPartWords = 16 * kWave + 16;    // 8-byte words of 16 columns' partial result: accumulators, then a maximum and a sum a column
+constexpr float kLowest = -3.0e38f, kSlack = 8.f, kHead = 36.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr u32 kNoTile = 0xffffffffu;
-using q8::i32x4;
-
-__device__ __forceinline__ i32x4 load_codes(const unsigned char* p) { return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p)); }
-__device__ __forceinline__ i32x4 load_scales(const unsigned char* p) { return *reinterpret_cast<const i32x4*>(p); }
 
 struct AttnArgs {
   const uint16_t* q;
@@ -53,8 +46,8 @@ struct AttnArgs {
   u64* part;
   int32_t* ticket;
   int B, NP, T, H, G, P, NB, R, W, window;
-  u32 page_magic;                              // ceil(2^32 / tiles of a page)
-  float scale_log2, cap_in, cap_out;           // logits in powers of two: s * scale_log2, or cap_out * tanh(s * cap_in)
+  u32 page_magic;                              // ceil(2^32 / tiles of a page), for pages of several
+  float scale_log2, cap_in, cap_out;           // logits in powers of two: s * scale_log2, or cap_out * tanh(s * cap_in / 2 log2 e)
 };
 
 template <int N, class F>
@@ -64,13 +57,21 @@ __device__ __forceinline__ void each_of(F f) {
     f(std::integral_constant<int, N - 1>{});
   }
 }
+__device__ __forceinline__ i32x4 load_codes(const unsigned char* p) { return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p)); }
+__device__ __forceinline__ i32x4 load_scales(const unsigned char* p) { return *reinterpret_cast<const i32x4*>(p); }
 __device__ __forceinline__ u64 pack_floats(float a, float b) { return (u64)as_u32(b) << 32 | as_u32(a); }
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ float max_of_column(float x) {      // over the four lanes that have a column
   x = fmaxf(x, __shfl_xor(x, 16, kWave));
   return fmaxf(x, __shfl_xor(x, 32, kWave));
 }
+__device__ __forceinline__ float sum_of_column(float x) {
+  x += __shfl_xor(x, 16, kWave);
+  return x + __shfl_xor(x, 32, kWave);
+}
 __device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ u32 byte_of(u32 w, int i) { return w >> (8 * i) & 255; }
+
 // Eight codes to an operand, times the scale
 __device__ __forceinline__ bf16x8 widen(int codes, float scale) {
   const u32 w = (u32)codes;
@@ -93,99 +94,229 @@ __device__ __forceinline__ void parts(const float* x, bf16x8 (&to)[NP]) {
   if constexpr (NP > 1) to[1] = __builtin_bit_cast(bf16x8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
 }
 
-template <bool BF16, int NQ, int REP>
-struct Wave {
+// What any and what every column of a wave sees
+struct Seen {
+  int first, behind;                           // tiles that any column sees
+  int lo, hi;                                  // positions that every column sees
+};
+
+// Sixteen columns: lane (c, n) = (lane / 16, lane % 16) has elements 16 i + 4 c + 0..3 of column n in o[i]
+template <bool BF16>
+struct Columns {
   static constexpr int NP = BF16 ? 1 : 2;      // parts of bf16 that a number of q's type has
+  f32x4 o[8];
+  float m, l, slope;
+  int lo, hi, pos;                             // first and last position that the lane's column sees, its own
+  bf16x8 q[4][NP];                             // elements 32 c + 8 i + 0..7
+
+  __device__ __forceinline__ void clear() {
+    m = kLowest;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // Row r of the unit and head of its group, or (!ok) a column that is none
+  __device__ __forceinline__ void begin(const AttnArgs& a, const Unit& u, bool ok, int r, int head, int len, int prefix, int (&see)[4]) {
+    const int row = u.row0 + r;
+    pos = u.pos0 + r;
+    lo = 0x7fffffff;
+    hi = -1;
+    slope = 0.f;
+    uint4 raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+    if (ok) {
+      const uint16_t* src = a.q + (long long)row * a.q_stride + (u.h * a.G + head) * kHeadDim + (threadIdx.x % kWave >> 4) * 32;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const uint4*>(src + i * 8);
+      lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+      if (a.row_from) lo = max(lo, a.row_from[row]);
+      hi = min(max(pos, prefix - 1), len - 1);
+      if (a.slopes) slope = a.slopes[u.h * a.G + head] * kLog2e;
+      see[0] = min(see[0], lo);
+      see[1] = max(see[1], hi);
+      see[2] = max(see[2], lo);
+      see[3] = min(see[3], hi);
+    }
+    float off = 0.f;                           // a row with an infinity or a NaN gives NaN, and no other row does
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float f[8];
+      cvt8<BF16>(raw[i], f);
+#pragma unroll
+      for (int y = 0; y < 8; ++y) off += f[y] * 0.f;
+      parts<NP>(f, q[i]);
+    }
+    if (!(sum_of_column(off) == 0.f))
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i][0] = __builtin_bit_cast(bf16x8, make_uint4(~0u, ~0u, ~0u, ~0u));
+    clear();
+  }
+  // Products of N x 4 tokens to logits in powers of two; at(j): the position of the first four of s[j]
+  template <int N, class At>
+  __device__ __forceinline__ void logits(const AttnArgs& a, f32x4 (&s)[N], At at) const {
+    if (a.cap_in != 0.f) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {          // tanh x = 1 - 2 / (e^2x + 1)
+          const float e = __builtin_amdgcn_exp2f(s[j][i] * a.cap_in);
+          s[j][i] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(e + 1.f);
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) s[j] *= a.scale_log2;
+    }
+    if (a.slopes) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[j][i] -= slope * fabsf((float)(pos - (at(j) + i)));
+    }
+  }
+  // Hides what the column does not see, and tiles that are none
+  template <int N, class At, class None>
+  __device__ __forceinline__ void hide(f32x4 (&s)[N], At at, None none) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (none(j) || at(j) + i < lo || at(j) + i > hi) s[j][i] = -INFINITY;
+  }
+  // Logits to weights
+  template <int N>
+  __device__ __forceinline__ void soften(f32x4 (&s)[N], float (&p)[4 * N]) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < N; ++j) mx = max3(max3(mx, s[j][0], s[j][1]), s[j][2], s[j][3]);
+    if (__any(mx > m - (kHead - kSlack))) {
+      mx = max_of_column(mx);
+      // (a column that does not need it stays, so that no row's result depends on its neighbours)
+      const float to = mx > m - (kHead - kSlack) ? mx + kHead : m, down = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= down;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] *= down;
+    }
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[4 * j + i] = __builtin_amdgcn_exp2f(s[j][i] - m);
+        sum[i] += p[4 * j + i];
+      }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  }
+  // Another partial result's accumulators joined to these.  lane_of(i): who had o[i], col: its maximum and sum's place
+  template <class Lane>
+  __device__ __forceinline__ void join(const u64* part, int col, Lane lane_of) {
+    const u64 ml = load_agent(part + 16 * kWave + col);
+    u64 y[8][2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      y[i][0] = load_agent(part + i * 2 * kWave + lane_of(i));
+      y[i][1] = load_agent(part + (i * 2 + 1) * kWave + lane_of(i));
+    }
+    const float l2 = as_f32((u32)(ml >> 32)), m2 = l2 == 0.f ? kLowest : as_f32((u32)ml);
+    const float to = fmaxf(m, m2), f1 = __builtin_amdgcn_exp2f(m - to), f2 = l2 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m2 - to);
+    m = to;
+    l = l * f1 + l2 * f2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const f32x4 z = {as_f32((u32)y[i][0]), as_f32((u32)(y[i][0] >> 32)), as_f32((u32)y[i][1]), as_f32((u32)(y[i][1] >> 32))};
+      o[i] = o[i] * f1 + z * f2;
+    }
+  }
+};
+
+__device__ __forceinline__ Seen seen_of(int (&see)[4]) {
+#pragma unroll
+  for (int x = 1; x < kWave; x <<= 1) {
+    see[0] = min(see[0], __shfl_xor(see[0], x, kWave));
+    see[1] = max(see[1], __shfl_xor(see[1], x, kWave));
+    see[2] = max(see[2], __shfl_xor(see[2], x, kWave));
+    see[3] = min(see[3], __shfl_xor(see[3], x, kWave));
+  }
+  Seen s;
+  s.first = __builtin_amdgcn_readfirstlane(see[0]) / kTile;
+  s.behind = (__builtin_amdgcn_readfirstlane(see[1]) + kTile) / kTile;
+  s.lo = __builtin_amdgcn_readfirstlane(see[2]);
+  s.hi = __builtin_amdgcn_readfirstlane(see[3]);
+  return s;
+}
+
+// N elements of a column's result over all tokens
+template <bool BF16, int N>
+__device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, int head, int d, const float (&v)[N], float m, float l) {
+  const size_t at = (size_t)(u.row0 + r) * a.H * a.G + u.h * a.G + head;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  u32 w[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) w[i] = pack2<BF16>(l == 0.f ? 0.f : v[2 * i] * inv, l == 0.f ? 0.f : v[2 * i + 1] * inv);
+  if constexpr (N == 8) *reinterpret_cast<uint4*>(a.out + at * kHeadDim + d) = make_uint4(w[0], w[1], w[2], w[3]);
+  else *reinterpret_cast<uint2*>(a.out + at * kHeadDim + d) = make_uint2(w[0], w[1]);
+  if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// Tiles of a sequence's pages
+struct Tiles {
+  const AttnArgs& a;
+  const Unit& u;
+  const int tpp;
+  __device__ __forceinline__ Tiles(const AttnArgs& a_, const Unit& u_) : a(a_), u(u_), tpp(a_.P / kTile) {}
+  __device__ __forceinline__ int page_of(int t) const { return tpp == 1 ? t : (int)__umulhi(t, a.page_magic); }
+  __device__ __forceinline__ int block(int t) const { return a.table[(size_t)u.seq * a.NP + page_of(t)]; }
+  // Place of tile t, whose page has this block, in lines of 128 bytes; none behind t1 or of a block that is none
+  __device__ __forceinline__ u32 line(int t, int t1, int b) const {
+    const int sub = t - page_of(t) * tpp;
+    return t < t1 && (unsigned)b < (unsigned)a.NB ? (((u32)b * a.H + u.h) * tpp + sub) * (kTileBytes / 128) : kNoTile;
+  }
+};
+// The pool's first tile where there is none: what is read there is hidden
+__device__ __forceinline__ const unsigned char* tile_at(const AttnArgs& a, u32 line) { return a.pages + (size_t)(line == kNoTile ? 0u : line) * 128; }
+
+// ---- few rows
+
+// A wave's 128 tokens at a time.  Values' scales are one for 32 elements of a token, which the second product sums over: they go into the
+// weights, so that each group of 32 columns of V has weights of its own, p * 2^e.  Where columns would be empty they repeat the
+// rows (REP): each copy weighs the values of a fraction of the groups.  CG waves share tokens and have 16 columns each.
+template <bool BF16, int REP, int CG>
+struct Wave {
+  static constexpr int NP = Columns<BF16>::NP;
   static constexpr int kCols = 16 / REP;       // columns that differ
   static constexpr int kGroups = 4 / REP;      // of V's groups of 32 columns, those that a lane weighs
-  static_assert(NQ == 1 || REP == 1, "");
-  f32x4 o[NQ][8];
-  float m[NQ], l[NQ], slope[NQ];
-  bf16x8 q[NQ][4][NP];
-  int lo[NQ], hi[NQ], pos[NQ];                 // first and last position that the lane's column sees, its own
-  int lo_most, hi_least;                       // what every column sees lies between
-  int t_first, t_behind;                       // tiles that any column sees
+  static_assert(CG == 1 || REP == 1, "");
+  Columns<BF16> x;
+  Seen seen;
 
   const AttnArgs& a;
-  const int lane, c, n, tpp;
+  const int lane, c, n, cg;                    // cg: which columns of the unit are the wave's
   Unit u;
 
   __device__ __forceinline__ Wave(const AttnArgs& a_)
-      : a(a_), lane(threadIdx.x % kWave), c((threadIdx.x % kWave) >> 4), n(threadIdx.x & 15), tpp(a_.P / kTile) {}
+      : a(a_), lane(threadIdx.x % kWave), c((threadIdx.x % kWave) >> 4), n(threadIdx.x & 15),
+        cg(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) % CG) {}
 
-  // Row of the unit and head of the group of column n + 16 g
-  __device__ __forceinline__ void column(int g, int& r, int& head) const {
-    const int col = REP > 1 ? n % kCols : n + 16 * g;
+  // Row of the unit and head of the group of column col
+  __device__ __forceinline__ bool column(int col, int& r, int& head) const {
     r = col / a.G;
     head = col - r * a.G;
+    return r < u.rows && r < a.R;
   }
-  __device__ __forceinline__ bool real(int r, int head) const { return head < a.G && r < u.rows; }
   // whether this lane's accumulators of 16 columns of V are of the weights that were made for them
   __device__ __forceinline__ bool has(int i) const { return REP == 1 || (i >> 1) % REP == n / kCols; }
+  // Lane that has column col's accumulators of 16 columns of V
+  __device__ __forceinline__ int lane_of(int i, int col, int quarter) const { return quarter * 16 + (REP == 1 ? col : col % kCols + (i >> 1) % REP * kCols); }
 
   __device__ __forceinline__ void begin(const Unit& unit) {
     u = unit;
     const int len = min(max(a.kv_len[u.seq], 0), a.NP * a.P);
     const int prefix = a.prefix_len ? min(a.prefix_len[u.seq], len) : 0;
-    int lo_min = 0x7fffffff, hi_max = -1;
-    lo_most = 0;
-    hi_least = 0x7fffffff;
-#pragma unroll
-    for (int g = 0; g < NQ; ++g) {
-      int r, head;
-      column(g, r, head);
-      const bool ok = real(r, head);
-      const int row = u.row0 + r;
-      pos[g] = u.pos0 + r;
-      lo[g] = 0x7fffffff;
-      hi[g] = -1;
-      slope[g] = 0.f;
-      uint4 raw[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) raw[i] = make_uint4(0, 0, 0, 0);
-      if (ok) {
-        const uint16_t* src = a.q + (long long)row * a.q_stride + (u.h * a.G + head) * kHeadDim + c * 32;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const uint4*>(src + i * 8);
-        lo[g] = a.window > 0 ? max(pos[g] - a.window + 1, 0) : 0;
-        if (a.row_from) lo[g] = max(lo[g], a.row_from[row]);
-        hi[g] = min(max(pos[g], prefix - 1), len - 1);
-        if (a.slopes) slope[g] = a.slopes[u.h * a.G + head] * kLog2e;
-        lo_min = min(lo_min, lo[g]);
-        hi_max = max(hi_max, hi[g]);
-        lo_most = max(lo_most, lo[g]);
-        hi_least = min(hi_least, hi[g]);
-      }
-      float off = 0.f;                         // a row with an infinity or a NaN gives NaN, and no other row does
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float f[8];
-        cvt8<BF16>(raw[i], f);
-#pragma unroll
-        for (int y = 0; y < 8; ++y) off += f[y] * 0.f;
-        parts<NP>(f, q[g][i]);
-      }
-      off += __shfl_xor(off, 16, kWave);
-      off += __shfl_xor(off, 32, kWave);
-      if (off != 0.f)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[g][i][0] = __builtin_bit_cast(bf16x8, make_uint4(~0u, ~0u, ~0u, ~0u));
-      m[g] = kLowest;
-      l[g] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-#pragma unroll
-    for (int x = 1; x < kWave; x <<= 1) {
-      lo_min = min(lo_min, __shfl_xor(lo_min, x, kWave));
-      lo_most = max(lo_most, __shfl_xor(lo_most, x, kWave));
-      hi_max = max(hi_max, __shfl_xor(hi_max, x, kWave));
-      hi_least = min(hi_least, __shfl_xor(hi_least, x, kWave));
-    }
-    t_first = __builtin_amdgcn_readfirstlane(lo_min) / kTile;
-    t_behind = (__builtin_amdgcn_readfirstlane(hi_max) + kTile) / kTile;
-    lo_most = __builtin_amdgcn_readfirstlane(lo_most);
-    hi_least = __builtin_amdgcn_readfirstlane(hi_least);
+    int see[4] = {0x7fffffff, -1, 0, 0x7fffffff}, r, head;
+    const bool ok = column(cg * 16 + n % kCols, r, head);
+    x.begin(a, u, ok, r, head, len, prefix, see);
+    seen = seen_of(see);
   }
 
   // ---- what is on its way
@@ -193,28 +324,10 @@ struct Wave {
   i32x4 k[8], v[8];
   u32 ks[2];
   i32x4 vs[kGroups][2];
-  u32 line, line_next;                         // of the step's tile lane % 8: its place in lines of 128 bytes, or none
+  u32 line, line_next;                         // of the step's tile lane % 8
   int block_next;                              // of the step after that
 
-  // The block of tile t0 + lane % 8, of those before t1
-  __device__ __forceinline__ int block_of(int t0, int t1) const {
-    const int t = t0 + (lane & 7);
-    int b = -1;
-    if (t < t1) {
-      const u32 page = tpp == 1 ? t : __umulhi(t, a.page_magic);
-      b = a.table[(size_t)u.seq * a.NP + page];
-    }
-    return b;
-  }
-  __device__ __forceinline__ u32 line_of(int t0, int b) const {
-    const int t = t0 + (lane & 7), sub = tpp == 1 ? 0 : t - (int)__umulhi(t, a.page_magic) * tpp;
-    return (unsigned)b < (unsigned)a.NB ? (((u32)b * a.H + u.h) * tpp + sub) * (kTileBytes / 128) : kNoTile;
-  }
-  // Tile i of the step; the pool's first where there is none (what is read there is hidden)
-  __device__ __forceinline__ const unsigned char* tile(u32 lines, int i) const {
-    const u32 x = __shfl(lines, i, kWave);
-    return a.pages + (size_t)(x == kNoTile ? 0u : x) * 128;
-  }
+  __device__ __forceinline__ const unsigned char* tile(u32 lines, int i) const { return tile_at(a, __shfl(lines, i, kWave)); }
   __device__ __forceinline__ void load_keys(u32 lines) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -227,307 +340,181 @@ struct Wave {
   __device__ __forceinline__ void load_values(u32 lines) {
     const unsigned char *at0 = tile(lines, 2 * c), *at1 = tile(lines, 2 * c + 1);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      v[2 * x] = load_codes(at0 + kValues + n * 16 + x * 256);
-      v[2 * x + 1] = load_codes(at1 + kValues + n * 16 + x * 256);
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = load_codes(at0 + kValues + n * 16 + i * 256);
+      v[2 * i + 1] = load_codes(at1 + kValues + n * 16 + i * 256);
     }
 #pragma unroll
-    for (int x = 0; x < kGroups; ++x) {
-      const int group = x * REP + (REP > 1 ? n / kCols : 0);
-      vs[x][0] = load_scales(at0 + kValueScales + group * 16);
-      vs[x][1] = load_scales(at1 + kValueScales + group * 16);
+    for (int i = 0; i < kGroups; ++i) {
+      const int group = i * REP + (REP > 1 ? n / kCols : 0);
+      vs[i][0] = load_scales(at0 + kValueScales + group * 16);
+      vs[i][1] = load_scales(at1 + kValueScales + group * 16);
     }
   }
 
   // ---- the step of tiles [t0, t0 + 8)
 
   // Row r of the products of tile j is token 32 (r / 4) + 4 j + r % 4 of the step, so that lane (c, n) gets tokens 32 c + 0..31 of column n
-  __device__ __forceinline__ void scores(f32x4 (&s)[NQ][8]) {
+  __device__ __forceinline__ void scores(f32x4 (&s)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float scale = two_to((int)(ks[j / 4] >> (8 * (j % 4)) & 255) - kBias);
-#pragma unroll
-      for (int g = 0; g < NQ; ++g) s[g][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float scale = two_to((int)byte_of(ks[j / 4], j % 4) - kBias);
+      s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const bf16x8 A = widen(k[j][i], scale);
 #pragma unroll
-        for (int g = 0; g < NQ; ++g)
-#pragma unroll
-          for (int p = 0; p < NP; ++p) s[g][j] = mfma32(A, q[g][i][p], s[g][j]);
+        for (int p = 0; p < NP; ++p) s[j] = mfma32(A, x.q[i][p], s[j]);
       }
     }
-  }
-  // Products to logits in powers of two, -infinity where the column does not see the token
-  __device__ __forceinline__ void logits(int g, int t0, f32x4 (&s)[8]) {
-    const int base = t0 * kTile, at = base + c * 32;
-    if (a.cap_in != 0.f) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {          // tanh x = 1 - 2 / (e^2x + 1)
-          const float e = __builtin_amdgcn_exp2f(s[j][i] * a.cap_in);
-          s[j][i] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(e + 1.f);
-        }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] *= a.scale_log2;
-    }
-    if (a.slopes) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[j][i] -= slope[g] * fabsf((float)(pos[g] - (at + j * 4 + i)));
-    }
-    if (base < lo_most || base + kStep * kTile - 1 > hi_least || __any(line == kNoTile)) {
-      const bool none[2] = {__shfl(line, 2 * c, kWave) == kNoTile, __shfl(line, 2 * c + 1, kWave) == kNoTile};
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = at + j * 4 + i;
-          if (none[j >> 2] || t < lo[g] || t > hi[g]) s[j][i] = -INFINITY;
-        }
-    }
-  }
-  __device__ __forceinline__ void soften(int g, f32x4 (&s)[8], float (&p)[32]) {
-    float mx = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) mx = max3(max3(mx, s[j][0], s[j][1]), s[j][2], s[j][3]);
-    if (__any(mx > m[g] - (kHead - kSlack))) {
-      mx = max_of_column(mx);
-      // (a column that does not need it stays, so that no row's result depends on its neighbours)
-      const float to = mx > m[g] - (kHead - kSlack) ? mx + kHead : m[g], down = __builtin_amdgcn_exp2f(m[g] - to);
-      m[g] = to;
-      l[g] *= down;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[g][i] *= down;
-    }
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[4 * j + i] = __builtin_amdgcn_exp2f(s[j][i] - m[g]);
-        sum[i] += p[4 * j + i];
-      }
-    l[g] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
   // What the tokens add to 32 columns of V (REP > 1: to REP groups of them, of which one has this lane's weights)
   template <int X>
-  __device__ __forceinline__ void weigh(const float (&p)[NQ][32]) {
+  __device__ __forceinline__ void weigh(const float (&p)[32]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {              // eight of the lane's tokens
-      bf16x8 B[NQ][NP];
+      bf16x8 B[NP];
+      float w[8];
 #pragma unroll
-      for (int g = 0; g < NQ; ++g) {
-        float w[8];
-#pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          const u32 word = vs[X][i >> 1][(i & 1) * 2 + (y >> 2)];
-          w[y] = __builtin_amdgcn_ldexpf(p[g][8 * i + y], (int)(word >> (8 * (y & 3)) & 255) - (kBias + kDown));
-        }
-        parts<NP>(w, B[g]);
-      }
+      for (int y = 0; y < 8; ++y)
+        w[y] = __builtin_amdgcn_ldexpf(p[8 * i + y], (int)byte_of(vs[X][i >> 1][(i & 1) * 2 + (y >> 2)], y & 3) - kBias);
+      parts<NP>(w, B);
 #pragma unroll
       for (int z = 0; z < 2 * REP; ++z) {
         const int d = X * 2 * REP + z;         // 16 columns
         const bf16x8 A = widen(v[d / 2 * 2 + (i >> 1)][d % 2 * 2 + (i & 1)], 1.f);
 #pragma unroll
-        for (int g = 0; g < NQ; ++g)
-#pragma unroll
-          for (int y = 0; y < NP; ++y) o[g][d] = mfma32(A, B[g][y], o[g][d]);
+        for (int y = 0; y < NP; ++y) x.o[d] = mfma32(A, B[y], x.o[d]);
       }
     }
   }
 
   // Tiles [from, to) of the unit.  Keys of the next step are asked for when those of this one have been taken, values likewise;
-  // the blocks of the tiles two steps ahead.
+  // the blocks of the tiles two steps ahead.  (Behind the last step too, where there is no tile: a wait counts the loads behind
+  // what it waits for, and has to find as many whichever way the code came.)
   __device__ __forceinline__ void sweep(int from, int to) {
     if (from < to) {
-      line = line_of(from, block_of(from, to));
-      block_next = block_of(from + kStep, to);
+      const Tiles tiles(a, u);
+      const int t8 = lane & 7, last = to - 1;
+      line = tiles.line(from + t8, to, tiles.block(min(from + t8, last)));
+      block_next = tiles.block(min(from + kStep + t8, last));
       load_keys(line);
       load_values(line);
       for (int t = from; t < to; t += kStep) {
-        const bool more = t + kStep < to;
-        f32x4 s[NQ][8];
+        f32x4 s[8];
         scores(s);
-        if (more) {
-          __builtin_amdgcn_sched_barrier(0);
-          line_next = line_of(t + kStep, block_next);
-          block_next = block_of(t + 2 * kStep, to);
-          load_keys(line_next);
-          __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);
+        line_next = tiles.line(t + kStep + t8, to, block_next);
+        block_next = tiles.block(min(t + 2 * kStep + t8, last));
+        load_keys(line_next);
+        __builtin_amdgcn_sched_barrier(0);
+        const int base = t * kTile;
+        auto at = [&](int j) { return base + c * 32 + j * 4; };
+        x.logits(a, s, at);
+        if (base < seen.lo || base + kStep * kTile - 1 > seen.hi || __any(line == kNoTile)) {
+          const bool none[2] = {__shfl(line, 2 * c, kWave) == kNoTile, __shfl(line, 2 * c + 1, kWave) == kNoTile};
+          x.hide(s, at, [&](int j) { return none[j >> 2]; });
         }
-        float p[NQ][32];
-#pragma unroll
-        for (int g = 0; g < NQ; ++g) {
-          logits(g, t, s[g]);
-          soften(g, s[g], p[g]);
-        }
-        each_of<kGroups>([&](auto x) { weigh<decltype(x)::value>(p); });
-        if (more) {
-          __builtin_amdgcn_sched_barrier(0);
-          line = line_next;
-          load_values(line);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        float p[32];
+        x.soften(s, p);
+        each_of<kGroups>([&](auto g) { weigh<decltype(g)::value>(p); });
+        __builtin_amdgcn_sched_barrier(0);
+        line = line_next;
+        load_values(line);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    // a column's four lanes have a quarter of its sum each
-#pragma unroll
-    for (int g = 0; g < NQ; ++g) {
-      l[g] += __shfl_xor(l[g], 16, kWave);
-      l[g] += __shfl_xor(l[g], 32, kWave);
-    }
+    x.l = sum_of_column(x.l);                  // a column's four lanes have a quarter of its sum each
   }
 
-  // Partial results of other workgroups, as this launch's lanes have them: accumulators [g][i][half][lane] in pairs, then
-  // (maximum, sum) [g][n]
-  __device__ __forceinline__ u64* part_of(int slot) const { return a.part + (size_t)slot * part_words(NQ); }
-  // Lane that has column n's accumulators of 16 columns of V
-  __device__ __forceinline__ int lane_of(int i, int col, int quarter) const { return quarter * 16 + (REP == 1 ? col : col % kCols + (i >> 1) % REP * kCols); }
-
-  // The joined results slot(from), slot(from + step), ... of `count`
-  template <class Slot>
-  __device__ __forceinline__ void gather(int from, int step, int count, Slot slot) {
-#pragma unroll
-    for (int g = 0; g < NQ; ++g) {
-      m[g] = kLowest;
-      l[g] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    for (int x = from; x < count; x += step) {
-      const u64* part = part_of(slot(x));
-#pragma unroll
-      for (int g = 0; g < NQ; ++g) {
-        const u64 ml = load_agent(part + NQ * 16 * kWave + g * 16 + n % kCols);
-        u64 y[8][2];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y[i][0] = load_agent(part + (g * 8 + i) * 2 * kWave + lane_of(i, n, c));
-          y[i][1] = load_agent(part + ((g * 8 + i) * 2 + 1) * kWave + lane_of(i, n, c));
-        }
-        const float l2 = as_f32((u32)(ml >> 32)), m2 = l2 == 0.f ? kLowest : as_f32((u32)ml);
-        const float to = fmaxf(m[g], m2), f1 = __builtin_amdgcn_exp2f(m[g] - to), f2 = l2 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m2 - to);
-        m[g] = to;
-        l[g] = l[g] * f1 + l2 * f2;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const f32x4 z = {as_f32((u32)y[i][0]), as_f32((u32)(y[i][0] >> 32)), as_f32((u32)y[i][1]), as_f32((u32)(y[i][1] >> 32))};
-          o[g][i] = o[g][i] * f1 + z * f2;
-        }
-      }
-    }
-  }
+  // Partial results of other workgroups, as this launch's lanes have them: accumulators [i][half][lane] in pairs, then (maximum, sum) [n]
+  __device__ __forceinline__ u64* part_of(int slot, int group) const { return a.part + ((size_t)slot * CG + group) * kPartWords; }
 };
 
-// A column's result over all tokens
-template <bool BF16, int N>
-__device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, int head, int d, const float (&v)[N], float m, float l) {
-  const size_t at = (size_t)(u.row0 + r) * a.H * a.G + u.h * a.G + head;
-  const float inv = l == 0.f ? 0.f : two_to(kDown) / l;
-  u32 w[N / 2];
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) w[i] = pack2<BF16>(l == 0.f ? 0.f : v[2 * i] * inv, l == 0.f ? 0.f : v[2 * i + 1] * inv);
-  if constexpr (N == 8) *reinterpret_cast<uint4*>(a.out + at * kHeadDim + d) = make_uint4(w[0], w[1], w[2], w[3]);
-  else *reinterpret_cast<uint2*>(a.out + at * kHeadDim + d) = make_uint2(w[0], w[1]);
-  if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-}
-
-template <int NQ>
 struct AttnLds {
-  float ml[kAttnWaves][16 * NQ][2];
+  float ml[kAttnWaves][16][2];
   __align__(16) float o[kAttnWaves][16][kColFloats];
   int last;
 };
 
-// The waves' results of one unit as one: with to_slot < 0 to the output, else there
-template <bool BF16, int NQ, int REP>
-__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, NQ, REP>& w, AttnLds<NQ>& lds, int to_slot) {
-  typedef Wave<BF16, NQ, REP> W;
+// The results of the waves that share columns as one: with to_slot < 0 to the output, else there
+template <bool BF16, int REP, int CG>
+__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, REP, CG>& w, AttnLds& lds, int to_slot) {
+  typedef Wave<BF16, REP, CG> W;
   const int tid = threadIdx.x, wave = tid / kWave;
   __syncthreads();                             // (what was there has been read)
-#pragma unroll
-  for (int g = 0; g < NQ; ++g)
-    if (w.c == 0) {
-      lds.ml[wave][g * 16 + w.n][0] = w.l[g] == 0.f ? kLowest : w.m[g];
-      lds.ml[wave][g * 16 + w.n][1] = w.l[g];
-    }
+  if (w.c == 0) {
+    lds.ml[wave][w.n][0] = w.x.l == 0.f ? kLowest : w.x.m;
+    lds.ml[wave][w.n][1] = w.x.l;
+  }
   __syncthreads();
+  float M = kLowest;
 #pragma unroll
-  for (int g = 0; g < NQ; ++g) {
-    float M = kLowest;
+  for (int i = 0; i < kAttnWaves; i += CG) M = fmaxf(M, lds.ml[i + w.cg][w.n][0]);
+  const float f = w.x.l == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.x.m - M);
 #pragma unroll
-    for (int i = 0; i < kAttnWaves; ++i) M = fmaxf(M, lds.ml[i][g * 16 + w.n][0]);
-    const float f = w.l[g] == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.m[g] - M);
-    if (g > 0) __syncthreads();
+  for (int i = 0; i < 8; ++i)
+    if (w.has(i)) *reinterpret_cast<f32x4*>(&lds.o[wave][w.n % W::kCols][i * 16 + w.c * 4]) = w.x.o[i] * f;
+  __syncthreads();
+  const int n = tid >> 4, d = (tid & 15) * 8;  // a column and eight of its elements
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (w.has(i)) *reinterpret_cast<f32x4*>(&lds.o[wave][w.n % W::kCols][i * 16 + w.c * 4]) = w.o[g][i] * f;
-    __syncthreads();
-    const int n = tid >> 4, d = (tid & 15) * 8;   // a column and eight of its elements
-    const int col = g * 16 + n, r = col / a.G, head = col - r * a.G;
-    if (n < W::kCols && w.real(r, head)) {
+  for (int g = 0; g < CG; ++g) {
+    int r, head;
+    if (n < W::kCols && w.column(g * 16 + n, r, head)) {
       float top = kLowest, L = 0.f, v[8];
 #pragma unroll
-      for (int i = 0; i < kAttnWaves; ++i) top = fmaxf(top, lds.ml[i][col][0]);
+      for (int i = g; i < kAttnWaves; i += CG) top = fmaxf(top, lds.ml[i][n][0]);
 #pragma unroll
-      for (int i = 0; i < kAttnWaves; ++i) {
-        const float l = lds.ml[i][col][1];
-        if (l != 0.f) L += l * __builtin_amdgcn_exp2f(lds.ml[i][col][0] - top);
+      for (int i = g; i < kAttnWaves; i += CG) {
+        const float l = lds.ml[i][n][1];
+        if (l != 0.f) L += l * __builtin_amdgcn_exp2f(lds.ml[i][n][0] - top);
       }
 #pragma unroll
       for (int y = 0; y < 8; ++y) {
         v[y] = 0.f;
 #pragma unroll
-        for (int i = 0; i < kAttnWaves; ++i) v[y] += lds.o[i][n][d + y];
+        for (int i = g; i < kAttnWaves; i += CG) v[y] += lds.o[i][n][d + y];
       }
       if (to_slot < 0) emit<BF16>(a, w.u, r, head, d, v, top, L);
       else {
-        u64* part = w.part_of(to_slot);
-        const int i = d / 16, at = (g * 8 + i) * 2 * kWave;
+        u64* part = w.part_of(to_slot, g);
+        const int i = d / 16;
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          store_agent(part + at + (y & 1) * kWave + w.lane_of(i, n, d % 16 / 4 + (y >> 1)), pack_floats(v[2 * y], v[2 * y + 1]));
-        if (d == 0) store_agent(part + NQ * 16 * kWave + col, pack_floats(top, L));
+          store_agent(part + (i * 2 + (y & 1)) * kWave + w.lane_of(i, n, d % 16 / 4 + (y >> 1)), pack_floats(v[2 * y], v[2 * y + 1]));
+        if (d == 0) store_agent(part + 16 * kWave + n, pack_floats(top, L));
       }
     }
   }
 }
 
-// Tiles [t0, t1) of a unit: by all waves, or, if they are one step, by wave `solo` alone.  Its result goes to the output if it is all of the
-// unit (count == 1), else to slot `mine` of the partial results, which the last of the `count` pieces to arrive joins, in
-// their order; slot(i) is the i-th one's number.
-template <bool BF16, int NQ, int REP, class Slot>
-__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, REP>& w, AttnLds<NQ>& lds, const Unit& u, int t0, int t1,
+// Tiles [t0, t1) of a unit: by all waves, or, if they are one step, by those of turn `solo` alone.  Its result goes to the output if it is
+// all of the unit (count == 1), else to slot `mine` of the partial results, which the last of the `count` pieces to arrive
+// joins, in their order; slot(i) is the i-th one's number.
+template <bool BF16, int REP, int CG, class Slot>
+__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, REP, CG>& w, AttnLds& lds, const Unit& u, int t0, int t1,
                                       int solo, int count, int mine, int ticket, Slot slot) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const bool alone = count == 1 && t1 - t0 <= kStep;   // (pieces of one unit are joined in one way, whichever comes last: the sums' order is fixed)
-  if (alone && wave != solo) return;
+  constexpr int kShares = kAttnWaves / CG;
+  const int share = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) / CG;
+  const bool alone = count == 1 && (t1 - t0 <= kStep || kShares == 1);     // (pieces of one unit are joined in one way, whichever comes last: the sums' order is fixed)
+  if (alone && share != solo % kShares) return;
   w.begin(u);
-  t0 = max(t0, w.t_first);
-  t1 = max(min(t1, w.t_behind), t0);
+  t0 = max(t0, w.seen.first);
+  t1 = max(min(t1, w.seen.behind), t0);
   if (!alone) {
-    const int per = ((t1 - t0 + kStep - 1) / kStep + kAttnWaves - 1) / kAttnWaves * kStep;
-    t0 = min(t0 + wave * per, t1);
+    const int per = ((t1 - t0 + kStep - 1) / kStep + kShares - 1) / kShares * kStep;
+    t0 = min(t0 + share * per, t1);
     t1 = min(t0 + per, t1);
   }
   w.sweep(t0, t1);
   if (alone) {
+    int r, head;
+    if (!w.column(w.cg * 16 + w.n % w.kCols, r, head)) return;
 #pragma unroll
-    for (int g = 0; g < NQ; ++g) {
-      int r, head;
-      w.column(g, r, head);
-      if (!w.real(r, head)) continue;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (!w.has(i)) continue;
-        const float v[4] = {w.o[g][i][0], w.o[g][i][1], w.o[g][i][2], w.o[g][i][3]};
-        emit<BF16>(a, u, r, head, i * 16 + w.c * 4, v, w.m[g], w.l[g]);
-      }
+    for (int i = 0; i < 8; ++i) {
+      if (!w.has(i)) continue;
+      const float v[4] = {w.x.o[i][0], w.x.o[i][1], w.x.o[i][2], w.x.o[i][3]};
+      emit<BF16>(a, u, r, head, i * 16 + w.c * 4, v, w.x.m, w.x.l);
     }
     return;
   }
@@ -541,30 +528,224 @@ __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, NQ, REP>& w,
   }
   __syncthreads();
   if (!lds.last) return;
-  w.gather(wave, kAttnWaves, count, slot);
+  w.x.clear();
+  for (int i = share; i < count; i += kShares)
+    w.x.join(w.part_of(slot(i), w.cg), w.n % w.kCols, [&](int y) { return w.lane_of(y, w.n, w.c); });
   merge_waves(a, w, lds, -1);
 }
 
-template <bool BF16, int NQ, int REP>
-__global__ __launch_bounds__(kAttnThreads, NQ == 2 ? 1 : 2) void q4_attn_kernel(AttnArgs a) {
-  __shared__ AttnLds<NQ> lds;
-  Wave<BF16, NQ, REP> w(a);
+// What a window leaves of a unit: tiles at most, and the first one
+__device__ __forceinline__ bool windowed(const AttnArgs& a) { return a.window > 0 && a.prefix_len == nullptr; }
+__device__ __forceinline__ int most_tiles(const AttnArgs& a) {
+  return windowed(a) ? (int)min(((long long)a.window + a.R + 2 * kTile - 3) / kTile, (long long)q8::kAllTiles) : q8::kAllTiles;
+}
+__device__ __forceinline__ int first_tile(const AttnArgs& a, const Unit& u) { return windowed(a) ? max(u.pos0 - a.window + 1, 0) / kTile : 0; }
+
+template <bool BF16, int REP, int CG>
+__global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
+  __shared__ AttnLds lds;
+  Wave<BF16, REP, CG> w(a);
   int solo = 0;
-  // what a window leaves of a unit begins at the tile of the first position that its first row sees
-  const bool windowed = a.window > 0 && a.prefix_len == nullptr;
-  const int most = windowed ? (int)min(((long long)a.window + a.R + 2 * kTile - 3) / kTile, (long long)q8::kAllTiles) : q8::kAllTiles;
-  deal<kAttnThreads, kLeastTiles>(a, false, most, [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
-    const int first = windowed ? max(u.pos0 - a.window + 1, 0) / kTile : 0;
+  deal<kAttnThreads, kLeastTiles, kPieceTiles>(a, false, most_tiles(a), [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
+    const int first = first_tile(a, u);
     piece(a, w, lds, u, first + t0, first + t1, solo, count, mine, f, slot);
-    solo = (solo + 1) % kAttnWaves;
+    ++solo;
   });
 }
 
-// Columns of 16 that the rows of a unit take, and how often they are repeated
-struct Shape { int groups, copies; };
+// ---- many rows
+
+// Each wave has its own kRowGroups * 16 columns, and the workgroup goes through the tokens together, 64 at a time: every wave fetches one
+// tile, widens it and puts it into LDS in operand order, while the 64 before it are taken; so a code is widened once for four
+// waves.  Values take their scales there.
+constexpr int kRowGroups = 2;
+constexpr int kStageTiles = kAttnWaves;
+struct RowsLds {
+  uint4 k[2][kStageTiles][4][kWave];           // [stage][tile][8 elements of 32][lane]
+  uint4 v[2][kStageTiles / 2][8][kWave];       // [stage][pair of tiles][16 elements][lane]
+  u32 line[2][kStageTiles];
+  int first[kAttnWaves], behind[kAttnWaves];
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs a) {
+  constexpr int NQ = kRowGroups, NP = Columns<BF16>::NP;
+  __shared__ RowsLds lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, c = lane >> 4, n = lane & 15;
+  const int rows = a.R / kAttnWaves;           // of a wave
+  Columns<BF16> x[NQ];
+  const bool grow = !windowed(a) && a.prefix_len == nullptr;
+  deal<kAttnThreads, kLeastTiles, 0>(a, grow, most_tiles(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
+    Unit u = whole;                            // this wave's rows
+    u.row0 += wave * rows;
+    u.pos0 += wave * rows;
+    u.rows = min(max(whole.rows - wave * rows, 0), rows);
+    const Tiles tiles(a, whole);
+    const int len = min(max(a.kv_len[u.seq], 0), a.NP * a.P);
+    const int prefix = a.prefix_len ? min(a.prefix_len[u.seq], len) : 0;
+    int see[4] = {0x7fffffff, -1, 0, 0x7fffffff};
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+      const int col = g * 16 + n, r = col / a.G;
+      x[g].begin(a, u, r < u.rows, r, col - r * a.G, len, prefix, see);
+    }
+    const Seen seen = seen_of(see);
+    __syncthreads();                           // (the last piece's stages have been read)
+    if (lane == 0) { lds.first[wave] = seen.first; lds.behind[wave] = seen.behind; }
+    __syncthreads();
+    const int first = first_tile(a, whole);
+    int from = lds.first[0], to = lds.behind[0];
+#pragma unroll
+    for (int i = 1; i < kAttnWaves; ++i) { from = min(from, lds.first[i]); to = max(to, lds.behind[i]); }
+    from = __builtin_amdgcn_readfirstlane(max(first + t0, from));
+    to = __builtin_amdgcn_readfirstlane(min(first + t1, to));
+
+    i32x4 kc, vc, vsc;                         // this wave's tile on its way: codes of keys and values, scales of values
+    u32 ksc = 0, line = kNoTile;
+    int block = -1;
+    auto fetch = [&](int t) {                  // tile t, whose block is at hand, and the block of the one after it
+      line = tiles.line(t, to, block);
+      block = tiles.block(min(t + kStageTiles, to - 1));
+      const unsigned char* at = tile_at(a, line);
+      kc = load_scales(at + n * 64 + c * 16);
+      vc = load_scales(at + kValues + lane * 16);
+      vsc = load_scales(at + kValueScales + c * 16);
+      ksc = at[kKeyScales + c * 16 + (n & 3) * 4 + (n >> 2)];
+    };
+    auto put = [&](int s) {
+      const float scale = two_to((int)ksc - kBias);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lds.k[s][wave][i][lane] = __builtin_bit_cast(uint4, widen(kc[i], scale));
+      // lane l has elements 32 (l / 16) + l % 16 and 16 more, 16 tokens each: two tokens of a byte, a scale each
+      u64* to_v = reinterpret_cast<u64*>(&lds.v[s][wave >> 1][2 * c][n]) + (wave & 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {            // tokens 4 i + 0..3, which are lane (i, n)'s
+        float e[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) e[y] = two_to((int)min(byte_of(vsc[i], y), (u32)(kExpMax + kBias)) - kBias);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const u32 w = (u32)vc[half * 2 + (i >> 1)];
+          u32 two[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            u32 lo, hi;
+            if ((i & 1) * 2 + y == 0) { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 0)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 0)); }
+            else if ((i & 1) * 2 + y == 1) { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 1)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 1)); }
+            else if ((i & 1) * 2 + y == 2) { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 2)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 2)); }
+            else { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 3)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 3)); }
+            two[y] = (lo & 0xffffu) | (hi & 0xffff0000u);
+          }
+          to_v[(half * kWave + i * 16) * 2] = (u64)two[1] << 32 | two[0];
+        }
+      }
+      if (lane == 0) lds.line[s][wave] = line;
+    };
+    if (from < to) {
+      block = tiles.block(min(from + wave, to - 1));
+      fetch(from + wave);
+      put(0);
+      __syncthreads();
+      int stage = 0;
+      for (int t = from; t < to; t += kStageTiles, stage ^= 1) {
+        fetch(t + kStageTiles + wave);
+        if (t < seen.behind && t + kStageTiles > seen.first) {
+          f32x4 s[NQ][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int g = 0; g < NQ; ++g) s[g][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const bf16x8 A = __builtin_bit_cast(bf16x8, lds.k[stage][j][i][lane]);
+#pragma unroll
+              for (int g = 0; g < NQ; ++g)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) s[g][j] = mfma32(A, x[g].q[i][p], s[g][j]);
+            }
+          }
+          const int base = t * kTile;
+          auto at = [&](int j) { return base + j * kTile + c * 4; };
+          u32 gone = 0;                        // bit j: tile j is none
+#pragma unroll
+          for (int j = 0; j < kStageTiles; ++j) gone |= lds.line[stage][j] == kNoTile ? 1u << j : 0u;
+          gone = __builtin_amdgcn_readfirstlane(gone);
+          const bool hide = base < seen.lo || base + kStageTiles * kTile - 1 > seen.hi || gone;
+          bf16x8 B[NQ][2][NP];
+#pragma unroll
+          for (int g = 0; g < NQ; ++g) {
+            x[g].logits(a, s[g], at);
+            if (hide) x[g].hide(s[g], at, [&](int j) { return (gone >> j & 1) != 0; });
+            float p[16];
+            x[g].soften(s[g], p);
+            parts<NP>(p, B[g][0]);
+            parts<NP>(p + 8, B[g][1]);
+          }
+#pragma unroll
+          for (int pair = 0; pair < 2; ++pair)
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+              const bf16x8 A = __builtin_bit_cast(bf16x8, lds.v[stage][pair][d][lane]);
+#pragma unroll
+              for (int g = 0; g < NQ; ++g)
+#pragma unroll
+                for (int y = 0; y < NP; ++y) x[g].o[d] = mfma32(A, B[g][pair][y], x[g].o[d]);
+            }
+        }
+        if (t + kStageTiles < to) {
+          put(stage ^ 1);
+          __syncthreads();
+        }
+      }
+    }
+    bool last = true;
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) x[g].l = sum_of_column(x[g].l);
+    if (count > 1) {
+      auto part_of = [&](int i, int g) { return a.part + (((size_t)i * kAttnWaves + wave) * NQ + g) * kPartWords; };
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) {
+        u64* part = part_of(mine, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          store_agent(part + i * 2 * kWave + lane, pack_floats(x[g].o[i][0], x[g].o[i][1]));
+          store_agent(part + (i * 2 + 1) * kWave + lane, pack_floats(x[g].o[i][2], x[g].o[i][3]));
+        }
+        if (c == 0) store_agent(part + 16 * kWave + n, pack_floats(x[g].m, x[g].l));
+      }
+      wave_drain_memory();                     // (written through and drained before the ticket, and read past the caches)
+      int before = 0;
+      if (lane == 0) before = __hip_atomic_fetch_add(a.ticket + f * kAttnWaves + wave, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = __builtin_amdgcn_readfirstlane(before) == count - 1;
+      if (last) {
+        if (lane == 0) store_agent(a.ticket + f * kAttnWaves + wave, 0);
+#pragma unroll
+        for (int g = 0; g < NQ; ++g) x[g].clear();
+        for (int i = 0; i < count; ++i)
+#pragma unroll
+          for (int g = 0; g < NQ; ++g) x[g].join(part_of(slot(i), g), n, [&](int) { return lane; });
+      }
+    }
+    if (last)
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) {
+        const int col = g * 16 + n, r = col / a.G;
+        if (r >= u.rows) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float v[4] = {x[g].o[i][0], x[g].o[i][1], x[g].o[i][2], x[g].o[i][3]};
+          emit<BF16>(a, u, r, col - r * a.G, i * 16 + c * 4, v, x[g].m, x[g].l);
+        }
+      }
+  });
+}
+
+// How the columns that the rows of a sequence take, on the average, are laid out: copies of them in 16, or groups of 16 (0: waves with
+// rows of their own)
+struct Shape { int copies, groups; };
 static Shape shape_of(int T, int B, int G) {
   const int64_t want = (int64_t)((T + B - 1) / B) * G;
-  return {want > 16 ? 2 : 1, want <= 4 ? 4 : want <= 8 ? 2 : 1};
+  return {want <= 4 ? 4 : want <= 8 ? 2 : 1, want <= 16 ? 1 : want <= 32 ? 2 : want <= 64 ? 4 : 0};
 }
 
 }  // namespace q4
@@ -573,8 +754,9 @@ static Shape shape_of(int T, int B, int G) {
 extern "C" int64_t kvd_q4_workspace_bytes(const kvd_q4_cache* c, const kvd_q8_rows* r) {
   using namespace kvd::q4;
   if (int e = check_cache(c, r)) return e;
-  static_assert(kAttnGroups * 4 <= kvd::q8::kTicketBytes, "a ticket for each workgroup");
-  return kvd::q8::kTicketBytes + (int64_t)kAttnGroups * 2 * 8 * part_words(shape_of(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads).groups);
+  static_assert(kAttnGroups * kAttnWaves * 4 <= kvd::q8::kTicketBytes, "a ticket for each wave of each workgroup");
+  const Shape shape = shape_of(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
+  return kvd::q8::kTicketBytes + (int64_t)kAttnGroups * 2 * 8 * kPartWords * (shape.groups ? shape.groups : kAttnWaves * kRowGroups);
 }
 
 extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const void* q, int64_t q_stride, const kvd_q4_scores* f,
@@ -614,19 +796,19 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
   const int tpp = a.P / kTile;
   a.page_magic = (kvd::u32)(((1ull << 32) + tpp - 1) / tpp);
   const Shape shape = shape_of(a.T, a.B, a.G);
-  a.R = 16 * shape.groups / shape.copies / a.G;
+  a.R = shape.groups ? 16 * shape.groups / shape.copies / a.G : 16 * kRowGroups / a.G * kAttnWaves;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.W), dim3(kAttnThreads), 0, s, a); };
-  if (c->kv_dtype == KVD_BF16) {
-    if (shape.groups == 2) go(q4_attn_kernel<true, 2, 1>);
-    else if (shape.copies == 4) go(q4_attn_kernel<true, 1, 4>);
-    else if (shape.copies == 2) go(q4_attn_kernel<true, 1, 2>);
-    else go(q4_attn_kernel<true, 1, 1>);
-  } else {
-    if (shape.groups == 2) go(q4_attn_kernel<false, 2, 1>);
-    else if (shape.copies == 4) go(q4_attn_kernel<false, 1, 4>);
-    else if (shape.copies == 2) go(q4_attn_kernel<false, 1, 2>);
-    else go(q4_attn_kernel<false, 1, 1>);
-  }
+  auto typed = [&](auto bf16) {
+    constexpr bool B = decltype(bf16)::value;
+    if (shape.copies == 4) go(q4_attn_kernel<B, 4, 1>);
+    else if (shape.copies == 2) go(q4_attn_kernel<B, 2, 1>);
+    else if (shape.groups == 1) go(q4_attn_kernel<B, 1, 1>);
+    else if (shape.groups == 2) go(q4_attn_kernel<B, 1, 2>);
+    else if (shape.groups == 4) go(q4_attn_kernel<B, 1, 4>);
+    else go(q4_attn_rows_kernel<B>);
+  };
+  if (c->kv_dtype == KVD_BF16) typed(std::true_type{});
+  else typed(std::false_type{});
   return launched();
 }

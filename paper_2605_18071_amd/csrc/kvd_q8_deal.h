@@ -21,46 +21,62 @@ __device__ __forceinline__ u64 uniform(u64 x) {
   return (u64)(u32)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (u32)__builtin_amdgcn_readfirstlane((int)x);
 }
 // The first unit of a sequence has `first` tiles and every next one `more` more, which is what their last rows see, rounded up.
-// `most` bounds the tiles of a unit; a.W workgroups (a multiple of kXcds) have LEAST tiles at least.
-template <int NT, int LEAST, class Args, class Each>
+// `most` bounds the tiles of a unit; a.W workgroups (a multiple of kXcds) have LEAST tiles at least.  ALIGN > 0: if the units are few
+// enough for a workgroup to each ALIGN tiles of one, that is how they are dealt out (not where they grow): then a unit of no more than
+// that needs no joining, which takes longer than its tiles.
+template <int NT, int LEAST, int ALIGN, class Args, class Each>
 __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Each each) {
   __shared__ u64 scan[NT / kWave];
   __shared__ u64 s_base;
   __shared__ int s_seq;
   const int tid = threadIdx.x, lane = tid % kWave, wv = tid / kWave;
   const int more = grow ? (a.R + kTile - 1) / kTile : 0;
+  int align = 1;                               // what a unit's tiles are rounded up to
   auto of = [&](int b, int& row0, int& rows, int& len, int& first) {   // returns units a head
     row0 = min(max(a.row_start[b], 0), a.T);
     rows = min(max(a.row_start[b + 1], row0), a.T) - row0;
     len = min(max(a.kv_len[b], 0), a.NP * a.P);
     first = min(max(((grow ? min(len, max(len - rows, 0) + a.R) : len) + kTile - 1) / kTile, 1), most);
+    if (ALIGN > 0) first = (first + align - 1) / align * align;
     return (rows + a.R - 1) / a.R;
   };
   // tiles of a sequence's first n units of a head
   auto upto_unit = [&](u64 n, int first) { return n * first + n * (n - 1) / 2 * more; };
   const int per = (a.B + NT - 1) / NT, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
-  u64 mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    int row0, rows, len, first;
-    const u64 units = of(b, row0, rows, len, first);
-    mine += upto_unit(units, first) * a.H;
-  }
-  u64 upto = mine;
+  u64 mine, upto, all;                         // tiles of this thread's sequences, up to their last, of all
+  auto count = [&] {
+    mine = all = 0;
+    for (int b = b0; b < b1; ++b) {
+      int row0, rows, len, first;
+      const u64 units = of(b, row0, rows, len, first);
+      mine += upto_unit(units, first) * a.H;
+    }
+    upto = mine;
 #pragma unroll
-  for (int x = 1; x < kWave; x <<= 1) {
-    const u64 y = ((u64)__shfl_up((u32)(upto >> 32), x, kWave) << 32) | __shfl_up((u32)upto, x, kWave);
-    if (lane >= x) upto += y;
-  }
-  if (lane == kWave - 1) scan[wv] = upto;
-  __syncthreads();
-  u64 all = 0;
+    for (int x = 1; x < kWave; x <<= 1) {
+      const u64 y = ((u64)__shfl_up((u32)(upto >> 32), x, kWave) << 32) | __shfl_up((u32)upto, x, kWave);
+      if (lane >= x) upto += y;
+    }
+    if (lane == kWave - 1) scan[wv] = upto;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NT / kWave; ++i) {
-    if (i < wv) upto += scan[i];
-    all += scan[i];
-  }
+    for (int i = 0; i < NT / kWave; ++i) {
+      if (i < wv) upto += scan[i];
+      all += scan[i];
+    }
+  };
+  if (ALIGN > 0 && !grow) {
+    align = ALIGN;
+    count();
+    if (all > (u64)a.W * ALIGN) {
+      align = 1;
+      __syncthreads();                         // (the sums have been read)
+      count();
+    }
+  } else count();
   u64 chunk = (all + a.W - 1) / a.W;
   if (chunk < (u64)LEAST) chunk = LEAST;
+  if (ALIGN > 0 && align > 1) chunk = ALIGN;
   // neighbours in the order of the units share keys and values: they go to one XCD, whose workgroups are every eighth, and its L2
   const int groups = (int)((all + chunk - 1) / chunk), each_xcd = (groups + kXcds - 1) / kXcds;
   if ((int)blockIdx.x / kXcds >= each_xcd) return;
