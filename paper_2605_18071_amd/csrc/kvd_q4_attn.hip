@@ -152,10 +152,12 @@ struct Columns {
       for (int i = 0; i < 4; ++i) q[i][0] = __builtin_bit_cast(bf16x8, make_uint4(~0u, ~0u, ~0u, ~0u));
     clear();
   }
-  // Products of N x 4 tokens to logits in powers of two; at(j): the position of the first four of s[j]
+  // Products of N x 4 tokens to logits in powers of two, but for the factor that is returned; at(j): the position of the first four of s[j]
   template <int N, class At>
-  __device__ __forceinline__ void logits(const AttnArgs& a, f32x4 (&s)[N], At at) const {
+  __device__ __forceinline__ float logits(const AttnArgs& a, f32x4 (&s)[N], At at) const {
+    float scale = a.scale_log2;
     if (a.cap_in != 0.f) {
+      scale = 1.f;
 #pragma unroll
       for (int j = 0; j < N; ++j)
 #pragma unroll
@@ -163,16 +165,15 @@ struct Columns {
           const float e = __builtin_amdgcn_exp2f(s[j][i] * a.cap_in);
           s[j][i] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(e + 1.f);
         }
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) s[j] *= a.scale_log2;
     }
     if (a.slopes) {
 #pragma unroll
       for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[j][i] -= slope * fabsf((float)(pos - (at(j) + i)));
+        for (int i = 0; i < 4; ++i) s[j][i] = s[j][i] * scale - slope * fabsf((float)(pos - (at(j) + i)));
+      scale = 1.f;
     }
+    return scale;
   }
   // Hides what the column does not see, and tiles that are none
   template <int N, class At, class None>
@@ -181,14 +182,15 @@ struct Columns {
     for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (none(j) || at(j) + i < lo || at(j) + i > hi) s[j][i] = -INFINITY;
+        if ((int)none(j) | (at(j) + i < lo) | (at(j) + i > hi)) s[j][i] = -INFINITY;
   }
-  // Logits to weights
+  // Logits, times `scale` > 0, to weights
   template <int N>
-  __device__ __forceinline__ void soften(f32x4 (&s)[N], float (&p)[4 * N]) {
+  __device__ __forceinline__ void soften(const f32x4 (&s)[N], float scale, float (&p)[4 * N]) {
     float mx = -INFINITY;
 #pragma unroll
     for (int j = 0; j < N; ++j) mx = max3(max3(mx, s[j][0], s[j][1]), s[j][2], s[j][3]);
+    mx *= scale;
     if (__any(mx > m - (kHead - kSlack))) {
       mx = max_of_column(mx);
       // (a column that does not need it stays, so that no row's result depends on its neighbours)
@@ -203,7 +205,7 @@ struct Columns {
     for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[4 * j + i] = __builtin_amdgcn_exp2f(s[j][i] - m);
+        p[4 * j + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][i], scale, -m));
         sum[i] += p[4 * j + i];
       }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -410,13 +412,13 @@ struct Wave {
         __builtin_amdgcn_sched_barrier(0);
         const int base = t * kTile;
         auto at = [&](int j) { return base + c * 32 + j * 4; };
-        x.logits(a, s, at);
+        const float scale = x.logits(a, s, at);
         if (base < seen.lo || base + kStep * kTile - 1 > seen.hi || __any(line == kNoTile)) {
           const bool none[2] = {__shfl(line, 2 * c, kWave) == kNoTile, __shfl(line, 2 * c + 1, kWave) == kNoTile};
           x.hide(s, at, [&](int j) { return none[j >> 2]; });
         }
         float p[32];
-        x.soften(s, p);
+        x.soften(s, scale, p);
         each_of<kGroups>([&](auto g) { weigh<decltype(g)::value>(p); });
         __builtin_amdgcn_sched_barrier(0);
         line = line_next;
@@ -488,15 +490,15 @@ __device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, 
   }
 }
 
-// Tiles [t0, t1) of a unit: by all waves, or, if they are one step, by those of turn `solo` alone.  Its result goes to the output if it is
+// Tiles [t0, t1) of a unit: by all waves, or, if they are one step (`step`), by those of turn `solo` alone.  Its result goes to the output if it is
 // all of the unit (count == 1), else to slot `mine` of the partial results, which the last of the `count` pieces to arrive
 // joins, in their order; slot(i) is the i-th one's number.
 template <bool BF16, int REP, int CG, class Slot>
 __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, REP, CG>& w, AttnLds& lds, const Unit& u, int t0, int t1,
-                                      int solo, int count, int mine, int ticket, Slot slot) {
+                                      bool step, int solo, int count, int mine, int ticket, Slot slot) {
   constexpr int kShares = kAttnWaves / CG;
   const int share = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) / CG;
-  const bool alone = count == 1 && (t1 - t0 <= kStep || kShares == 1);     // (pieces of one unit are joined in one way, whichever comes last: the sums' order is fixed)
+  const bool alone = count == 1 && (step || kShares == 1);     // (pieces of one unit are joined in one way, whichever comes last: the sums' order is fixed)
   if (alone && share != solo % kShares) return;
   w.begin(u);
   t0 = max(t0, w.seen.first);
@@ -539,16 +541,21 @@ __device__ __forceinline__ bool windowed(const AttnArgs& a) { return a.window > 
 __device__ __forceinline__ int most_tiles(const AttnArgs& a) {
   return windowed(a) ? (int)min(((long long)a.window + a.R + 2 * kTile - 3) / kTile, (long long)q8::kAllTiles) : q8::kAllTiles;
 }
-__device__ __forceinline__ int first_tile(const AttnArgs& a, const Unit& u) { return windowed(a) ? max(u.pos0 - a.window + 1, 0) / kTile : 0; }
+// Where its tiles are counted from: a unit's first piece has what lies before that too
+__device__ __forceinline__ int first_tile(const AttnArgs& a, const Unit& u) { return max(u.lead, windowed(a) ? max(u.pos0 - a.window + 1, 0) / kTile : 0); }
+// Tiles of a sequence that its first row does not see, and no other row as a rule
+__device__ __forceinline__ auto lead_of(const AttnArgs& a) {
+  return [&a](int row0) { return a.row_from && row0 < a.T ? max(a.row_from[row0], 0) / kTile : 0; };
+}
 
 template <bool BF16, int REP, int CG>
 __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
   __shared__ AttnLds lds;
   Wave<BF16, REP, CG> w(a);
   int solo = 0;
-  deal<kAttnThreads, kLeastTiles, kPieceTiles>(a, false, most_tiles(a), [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<kAttnThreads, kLeastTiles, kPieceTiles>(a, false, most_tiles(a), lead_of(a), [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
     const int first = first_tile(a, u);
-    piece(a, w, lds, u, first + t0, first + t1, solo, count, mine, f, slot);
+    piece(a, w, lds, u, t0 > 0 ? first + t0 : 0, first + t1, t1 - t0 <= kStep, solo, count, mine, f, slot);
     ++solo;
   });
 }
@@ -575,7 +582,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
   const int rows = a.R / kAttnWaves;           // of a wave
   Columns<BF16> x[NQ];
   const bool grow = !windowed(a) && a.prefix_len == nullptr;
-  deal<kAttnThreads, kLeastTiles, 0>(a, grow, most_tiles(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<kAttnThreads, kLeastTiles, 0>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
     u.row0 += wave * rows;
     u.pos0 += wave * rows;
@@ -597,7 +604,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
     int from = lds.first[0], to = lds.behind[0];
 #pragma unroll
     for (int i = 1; i < kAttnWaves; ++i) { from = min(from, lds.first[i]); to = max(to, lds.behind[i]); }
-    from = __builtin_amdgcn_readfirstlane(max(first + t0, from));
+    from = __builtin_amdgcn_readfirstlane(max(t0 > 0 ? first + t0 : 0, from));
     to = __builtin_amdgcn_readfirstlane(min(first + t1, to));
 
     i32x4 kc, vc, vsc;                         // this wave's tile on its way: codes of keys and values, scales of values
@@ -650,19 +657,29 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
       for (int t = from; t < to; t += kStageTiles, stage ^= 1) {
         fetch(t + kStageTiles + wave);
         if (t < seen.behind && t + kStageTiles > seen.first) {
+          // operands are asked for four at a time, while the four before them are taken: keys of two tiles, two of their four
+          // parts each, then values of a pair of tiles, four of their eight
+          uint4 b[2][4];
+          auto ask = [&](int i) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              b[i & 1][y] = i < 4 ? lds.k[stage][i / 2 * 2 + (y & 1)][i % 2 * 2 + (y >> 1)][lane] : lds.v[stage][i / 2 - 2][i % 2 * 4 + y][lane];
+            __builtin_amdgcn_sched_barrier(0);
+          };
+          ask(0);
           f32x4 s[NQ][4];
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int i = 0; i < 4; ++i) {
+            ask(i + 1);
 #pragma unroll
-            for (int g = 0; g < NQ; ++g) s[g][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const bf16x8 A = __builtin_bit_cast(bf16x8, lds.k[stage][j][i][lane]);
+              for (int p = 0; p < NP; ++p)
 #pragma unroll
-              for (int g = 0; g < NQ; ++g)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) s[g][j] = mfma32(A, x[g].q[i][p], s[g][j]);
-            }
+                for (int g = 0; g < NQ; ++g)
+                  s[g][i / 2 * 2 + (y & 1)] = mfma32(__builtin_bit_cast(bf16x8, b[i & 1][y]), x[g].q[i % 2 * 2 + (y >> 1)][p],
+                                                    i % 2 == 0 && y < 2 && p == 0 ? zero : s[g][i / 2 * 2 + (y & 1)]);
           }
           const int base = t * kTile;
           auto at = [&](int j) { return base + j * kTile + c * 4; };
@@ -674,23 +691,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
           bf16x8 B[NQ][2][NP];
 #pragma unroll
           for (int g = 0; g < NQ; ++g) {
-            x[g].logits(a, s[g], at);
+            const float scale = x[g].logits(a, s[g], at);
             if (hide) x[g].hide(s[g], at, [&](int j) { return (gone >> j & 1) != 0; });
             float p[16];
-            x[g].soften(s[g], p);
+            x[g].soften(s[g], scale, p);
             parts<NP>(p, B[g][0]);
             parts<NP>(p + 8, B[g][1]);
           }
 #pragma unroll
-          for (int pair = 0; pair < 2; ++pair)
+          for (int i = 0; i < 4; ++i) {
+            if (i < 3) ask(i + 5);
 #pragma unroll
-            for (int d = 0; d < 8; ++d) {
-              const bf16x8 A = __builtin_bit_cast(bf16x8, lds.v[stage][pair][d][lane]);
+            for (int y = 0; y < 4; ++y)
 #pragma unroll
-              for (int g = 0; g < NQ; ++g)
+              for (int p = 0; p < NP; ++p)
 #pragma unroll
-                for (int y = 0; y < NP; ++y) x[g].o[d] = mfma32(A, B[g][pair][y], x[g].o[d]);
-            }
+                for (int g = 0; g < NQ; ++g)
+                  x[g].o[i % 2 * 4 + y] = mfma32(__builtin_bit_cast(bf16x8, b[i & 1][y]), B[g][i / 2][p], x[g].o[i % 2 * 4 + y]);
+          }
         }
         if (t + kStageTiles < to) {
           put(stage ^ 1);
@@ -770,7 +788,7 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
   if (reinterpret_cast<uintptr_t>(lse) & 3) return KVD_ERR_ARG;
   if (!aligned(r->page_table, 4) || !aligned(r->kv_len, 4) || !aligned(r->row_start, 4)) return KVD_ERR_ARG;
   AttnArgs a = {};
-  a.scale_log2 = (c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e;
+  a.scale_log2 = fminf(fmaxf((c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e, 0x1p-126f), 0x1.fffffep127f);
   if (f) {
     if (!(f->softcap >= 0.f) || isinf(f->softcap)) return KVD_ERR_ARG;
     if (f->window < 0) return KVD_ERR_SHAPE;

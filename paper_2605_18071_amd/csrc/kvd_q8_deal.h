@@ -11,6 +11,7 @@ constexpr int kAllTiles = 1 << 30;             // no bound on a unit's tiles
 // What the rows of one unit (up to R rows of a sequence, one head) have in common
 struct Unit {
   int row0, rows, h, seq, pos0, entries;       // pos0: position of row0; entries: pages (or selected pages)
+  int lead;                                    // tiles in front of those that were counted
 };
 
 // All tokens.  The units' tiles, one unit behind the other, are dealt out evenly: workgroup i has tiles [i, i + 1) * chunk of
@@ -23,20 +24,24 @@ __device__ __forceinline__ u64 uniform(u64 x) {
 // The first unit of a sequence has `first` tiles and every next one `more` more, which is what their last rows see, rounded up.
 // `most` bounds the tiles of a unit; a.W workgroups (a multiple of kXcds) have LEAST tiles at least.  ALIGN > 0: if the units are few
 // enough for a workgroup to each ALIGN tiles of one, that is how they are dealt out (not where they grow): then a unit of no more than
-// that needs no joining, which takes longer than its tiles.
-template <int NT, int LEAST, int ALIGN, class Args, class Each>
-__device__ __forceinline__ void deal(const Args& a, bool grow, int most, Each each) {
+// that needs no joining, which takes longer than its tiles.  lead(row): tiles at the beginning of the sequence that begins with that
+// row which are left out of the count.
+template <int NT, int LEAST, int ALIGN, class Args, class Lead, class Each>
+__device__ __forceinline__ void deal(const Args& a, bool grow, int most, Lead lead, Each each) {
   __shared__ u64 scan[NT / kWave];
   __shared__ u64 s_base;
   __shared__ int s_seq;
   const int tid = threadIdx.x, lane = tid % kWave, wv = tid / kWave;
   const int more = grow ? (a.R + kTile - 1) / kTile : 0;
   int align = 1;                               // what a unit's tiles are rounded up to
+  int skip = 0;                                // lead of the sequence that was last asked for
   auto of = [&](int b, int& row0, int& rows, int& len, int& first) {   // returns units a head
     row0 = min(max(a.row_start[b], 0), a.T);
     rows = min(max(a.row_start[b + 1], row0), a.T) - row0;
     len = min(max(a.kv_len[b], 0), a.NP * a.P);
-    first = min(max(((grow ? min(len, max(len - rows, 0) + a.R) : len) + kTile - 1) / kTile, 1), most);
+    first = max(((grow ? min(len, max(len - rows, 0) + a.R) : len) + kTile - 1) / kTile, 1);
+    skip = rows > 0 ? min(lead(row0), first - 1) : 0;
+    first = min(first - skip, most);
     if (ALIGN > 0) first = (first + align - 1) / align * align;
     return (rows + a.R - 1) / a.R;
   };
@@ -107,6 +112,7 @@ __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Each ea
     rows = __builtin_amdgcn_readfirstlane(rows);
     len = __builtin_amdgcn_readfirstlane(len);
     first = __builtin_amdgcn_readfirstlane(first);
+    const int in_front = __builtin_amdgcn_readfirstlane(skip);
     const u64 end = base + upto_unit(units, first) * a.H;
     while (at < min(end, stop)) {
       // unit `part` of its head: the largest one that begins at or before `at`, a head's units one behind the other
@@ -123,6 +129,7 @@ __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Each ea
       const u64 begin = base + h * of_head + upto_unit(part, first);
       const int tiles = first + (int)part * more, t0 = (int)(at - begin), t1 = (int)min((u64)tiles, stop - begin);
       Unit u;
+      u.lead = in_front;
       u.seq = b;
       u.h = (int)h;
       u.row0 = row0 + (int)part * a.R;
