@@ -8,11 +8,11 @@
 // (The matrix cores' own products of 4-bit operands with scales take keys and values as they are, but their sums of eight products
 // keep 13 bits below the largest: logits of 140 came out 2^-16 off, and small weights beside a large one got lost.)
 //
-// One pass with a running reference m and sum l of a column: p = 2^(x - m).  m is kHead above the largest logit when it is set, and
-// is raised only when a logit passes that by more than kSlack, so that the accumulators are rarely touched; p then stays below
-// 2^(kSlack - kHead), so that 2^24 tokens' values of up to 2^128 have finite sums.
+// One pass with a running reference m and sum l of a column: p = 2^(x - m).  m is HEAD above the largest logit when it is set, and
+// is raised only when a logit passes that by more than kSlack, so that the accumulators are rarely touched.  What multiplies values
+// of up to 2^128 stays below 2^-28, so that 2^24 of them have finite sums.
 // bf16: weights are rounded to bf16, by 2^-8 of themselves at most, like their output.  f16, whose outputs would show it: a
-// second product takes what the rounding left (2^-17), and the first one has the queries in two parts of bf16 too.
+// second product takes what the rounding left (2^-16), and the first one has the queries in two parts of bf16 too.
 #include "kvd_q4.h"
 #include "kvd_q8_deal.h"
 
@@ -23,6 +23,7 @@ using q8::bf16x8;
 using q8::deal;
 using q8::i32x4;
 using q8::Unit;
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnGroups = 512;               // workgroups: two for each CU
@@ -31,7 +32,8 @@ constexpr int kLeastTiles = 32;                // tiles of a workgroup at least
 constexpr int kPieceTiles = 64;                // tiles of a workgroup where there are few
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 constexpr int kPartWords = 16 * kWave + 16;    // 8-byte words of 16 columns' partial result: accumulators, then a maximum and a sum a column
-constexpr float kLowest = -3.0e38f, kSlack = 8.f, kHead = 36.f;
+constexpr float kLowest = -3.0e38f, kSlack = 8.f;
+constexpr int kFewHead = -90, kRowsHead = 36, kFewDown = 126;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr u32 kNoTile = 0xffffffffu;
 
@@ -94,6 +96,20 @@ __device__ __forceinline__ void parts(const float* x, bf16x8 (&to)[NP]) {
   if constexpr (NP > 1) to[1] = __builtin_bit_cast(bf16x8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
 }
 
+// Eight weights, none of them negative, to NP operands whose parts are not negative either: rounded to bf16, or cut, and what that left
+template <int NP>
+__device__ __forceinline__ void weights(const float* p, u16x2 (&to)[NP][4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = p[2 * i], b = p[2 * i + 1];
+    if constexpr (NP == 1) to[0][i] = __builtin_bit_cast(u16x2, pack2<true>(a, b));
+    else {
+      to[0][i] = __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(as_u32(b), as_u32(a), 0x07060302));
+      to[1][i] = __builtin_bit_cast(u16x2, pack2<true>(a - as_f32(as_u32(a) & 0xffff0000u), b - as_f32(as_u32(b) & 0xffff0000u)));
+    }
+  }
+}
+
 // What any and what every column of a wave sees
 struct Seen {
   int first, behind;                           // tiles that any column sees
@@ -101,8 +117,9 @@ struct Seen {
 };
 
 // Sixteen columns: lane (c, n) = (lane / 16, lane % 16) has elements 16 i + 4 c + 0..3 of column n in o[i]
-template <bool BF16>
+template <bool BF16, int HEAD>
 struct Columns {
+  static constexpr float kHead = HEAD;
   static constexpr int NP = BF16 ? 1 : 2;      // parts of bf16 that a number of q's type has
   f32x4 o[8];
   float m, l, slope;
@@ -167,10 +184,11 @@ struct Columns {
         }
     }
     if (a.slopes) {
+      const float far = (float)(at(0) - pos);  // (below 2^24: exact, and its sums)
 #pragma unroll
       for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[j][i] = s[j][i] * scale - slope * fabsf((float)(pos - (at(j) + i)));
+        for (int i = 0; i < 4; ++i) s[j][i] = s[j][i] * scale - slope * fabsf(far + (float)(at(j) - at(0) + i));
       scale = 1.f;
     }
     return scale;
@@ -248,11 +266,11 @@ __device__ __forceinline__ Seen seen_of(int (&see)[4]) {
   return s;
 }
 
-// N elements of a column's result over all tokens
-template <bool BF16, int N>
+// N elements of a column's result over all tokens; the weights were taken times 2^-DOWN
+template <bool BF16, int DOWN, int N>
 __device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, int head, int d, const float (&v)[N], float m, float l) {
   const size_t at = (size_t)(u.row0 + r) * a.H * a.G + u.h * a.G + head;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = l == 0.f ? 0.f : two_to(DOWN) / l;
   u32 w[N / 2];
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) w[i] = pack2<BF16>(l == 0.f ? 0.f : v[2 * i] * inv, l == 0.f ? 0.f : v[2 * i + 1] * inv);
@@ -285,11 +303,11 @@ __device__ __forceinline__ const unsigned char* tile_at(const AttnArgs& a, u32 l
 // rows (REP): each copy weighs the values of a fraction of the groups.  CG waves share tokens and have 16 columns each.
 template <bool BF16, int REP, int CG>
 struct Wave {
-  static constexpr int NP = Columns<BF16>::NP;
+  static constexpr int NP = Columns<BF16, kFewHead>::NP;
   static constexpr int kCols = 16 / REP;       // columns that differ
   static constexpr int kGroups = 4 / REP;      // of V's groups of 32 columns, those that a lane weighs
   static_assert(CG == 1 || REP == 1, "");
-  Columns<BF16> x;
+  Columns<BF16, kFewHead> x;
   Seen seen;
 
   const AttnArgs& a;
@@ -370,17 +388,23 @@ struct Wave {
       }
     }
   }
-  // What the tokens add to 32 columns of V (REP > 1: to REP groups of them, of which one has this lane's weights)
+  // What the tokens add to 32 columns of V (REP > 1: to REP groups of them, of which one has this lane's weights).  p * 2^(e - 126): a
+  // bf16's bits less 126 - e in its exponent, which are those of a smaller number, and 0 where there would be none; p is up to 2^98.
   template <int X>
-  __device__ __forceinline__ void weigh(const float (&p)[32]) {
+  __device__ __forceinline__ void weigh(const u16x2 (&p)[4][NP][4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {              // eight of the lane's tokens
       bf16x8 B[NP];
-      float w[8];
+      u16x2 w[NP][4];
 #pragma unroll
-      for (int y = 0; y < 8; ++y)
-        w[y] = __builtin_amdgcn_ldexpf(p[8 * i + y], (int)byte_of(vs[X][i >> 1][(i & 1) * 2 + (y >> 2)], y & 3) - kBias);
-      parts<NP>(w, B);
+      for (int y = 0; y < 4; ++y) {
+        const u32 bytes = __builtin_amdgcn_perm(0, (u32)vs[X][i >> 1][(i & 1) * 2 + (y >> 1)], y & 1 ? 0x0c030c02 : 0x0c010c00);
+        const u16x2 down = (unsigned short)((kBias + kFewDown) << 7) - __builtin_bit_cast(u16x2, bytes) * (unsigned short)128;
+#pragma unroll
+        for (int z = 0; z < NP; ++z) w[z][y] = __builtin_elementwise_sub_sat(p[i][z][y], down);
+      }
+#pragma unroll
+      for (int z = 0; z < NP; ++z) B[z] = __builtin_bit_cast(bf16x8, w[z]);
 #pragma unroll
       for (int z = 0; z < 2 * REP; ++z) {
         const int d = X * 2 * REP + z;         // 16 columns
@@ -419,7 +443,10 @@ struct Wave {
         }
         float p[32];
         x.soften(s, scale, p);
-        each_of<kGroups>([&](auto g) { weigh<decltype(g)::value>(p); });
+        u16x2 w[4][NP][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) weights<NP>(p + 8 * i, w[i]);
+        each_of<kGroups>([&](auto g) { weigh<decltype(g)::value>(w); });
         __builtin_amdgcn_sched_barrier(0);
         line = line_next;
         load_values(line);
@@ -477,7 +504,7 @@ __device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, 
 #pragma unroll
         for (int i = g; i < kAttnWaves; i += CG) v[y] += lds.o[i][n][d + y];
       }
-      if (to_slot < 0) emit<BF16>(a, w.u, r, head, d, v, top, L);
+      if (to_slot < 0) emit<BF16, kFewDown>(a, w.u, r, head, d, v, top, L);
       else {
         u64* part = w.part_of(to_slot, g);
         const int i = d / 16;
@@ -516,7 +543,7 @@ __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, REP, CG>& w,
     for (int i = 0; i < 8; ++i) {
       if (!w.has(i)) continue;
       const float v[4] = {w.x.o[i][0], w.x.o[i][1], w.x.o[i][2], w.x.o[i][3]};
-      emit<BF16>(a, u, r, head, i * 16 + w.c * 4, v, w.x.m, w.x.l);
+      emit<BF16, kFewDown>(a, u, r, head, i * 16 + w.c * 4, v, w.x.m, w.x.l);
     }
     return;
   }
@@ -576,11 +603,11 @@ struct RowsLds {
 
 template <bool BF16>
 __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs a) {
-  constexpr int NQ = kRowGroups, NP = Columns<BF16>::NP;
+  constexpr int NQ = kRowGroups, NP = Columns<BF16, kRowsHead>::NP;
   __shared__ RowsLds lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, c = lane >> 4, n = lane & 15;
   const int rows = a.R / kAttnWaves;           // of a wave
-  Columns<BF16> x[NQ];
+  Columns<BF16, kRowsHead> x[NQ];
   const bool grow = !windowed(a) && a.prefix_len == nullptr;
   deal<kAttnThreads, kLeastTiles, 0>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
@@ -752,7 +779,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float v[4] = {x[g].o[i][0], x[g].o[i][1], x[g].o[i][2], x[g].o[i][3]};
-          emit<BF16>(a, u, r, col - r * a.G, i * 16 + c * 4, v, x[g].m, x[g].l);
+          emit<BF16, 0>(a, u, r, col - r * a.G, i * 16 + c * 4, v, x[g].m, x[g].l);
         }
       }
   });

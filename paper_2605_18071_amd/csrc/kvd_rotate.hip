@@ -11,6 +11,7 @@ constexpr int kRotThreads = 256;
 constexpr int kMaxPairs = kHeadDim / 2;
 constexpr int kMaxRotRows = 1 << 24;
 constexpr int kMaxRotHeads = 65536;
+constexpr int kAhead = 4;                      // heads on their way to 16 lanes
 
 struct RotateArgs {
   const uint16_t *q, *k, *q_weight, *k_weight;
@@ -21,6 +22,16 @@ struct RotateArgs {
   int T, Hq, Hk, pairs, axis_end[4];           // axis_end: first pair behind the axis
   float eps;
 };
+
+// Cosine and sine of r turns, r in -1/2..1/2: quarter turns taken off, then their series, off by 2^-25 where they end
+__device__ __forceinline__ float2 cos_sin(float r) {
+  const float quarters = rintf(4.f * r), x = 6.28318530717958648f * (r - 0.25f * quarters), x2 = x * x;     // |x| <= pi / 4
+  const float s = x + x * x2 * (-1.f / 6 + x2 * (1.f / 120 + x2 * (-1.f / 5040 + x2 * (1.f / 362880))));
+  const float c = 1.f + x2 * (-0.5f + x2 * (1.f / 24 + x2 * (-1.f / 720 + x2 * (1.f / 40320 + x2 * (-1.f / 3628800)))));
+  const int q = (int)quarters & 3;
+  const float a = q & 1 ? s : c, b = q & 1 ? c : s;
+  return make_float2(q == 1 || q == 2 ? -a : a, q & 2 ? -b : b);
+}
 
 // NR rows a workgroup; 16 lanes have a head, 8 elements each.  NEAR: a pair's elements are neighbours, else `pairs` apart.
 template <bool BF16, bool NEAR, int NR>
@@ -37,16 +48,18 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_kernel(RotateArgs a) 
     return h < a.Hq ? a.q + row * a.q_stride + (long long)h * kHeadDim + j * 8
                     : a.k + row * a.k_stride + (long long)(h - a.Hq) * kHeadDim + j * 8;
   };
-  uint4 x = make_uint4(0, 0, 0, 0);
-  if (real && head < heads) x = *reinterpret_cast<const uint4*>(at(head));
+  uint4 x[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (real && head + i * per < heads) x[i] = *reinterpret_cast<const uint4*>(at(head + i * per));
+  }
   for (int i = tid; i < NR * kMaxPairs; i += kRotThreads) {
     const int r = i / kMaxPairs, p = i % kMaxPairs;
     if (p < a.pairs && row0 + r < a.T) {
       const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
       const double turns = (double)a.pos[axis * a.pos_stride + row0 + r] * ((double)a.inv_freq[p] * 0.15915494309189533577);
-      float s, c;
-      sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-      turn[r][p] = make_float2(c, s);
+      turn[r][p] = cos_sin((float)(turns - rint(turns)));
     }
   }
   __syncthreads();
@@ -69,49 +82,53 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_kernel(RotateArgs a) 
     vk = *reinterpret_cast<const uint4*>(a.k_weight + (partner & 15) * 8);
   }
   if (!real) return;                           // (whole groups of 16 lanes)
-  for (; head < heads; head += per) {
-    const bool is_q = head < a.Hq, norm = (is_q ? a.q_weight : a.k_weight) != nullptr;
-    uint4 next = x;
-    if (head + per < heads) next = *reinterpret_cast<const uint4*>(at(head + per));
-    float f[8], g[8];
-    cvt8<BF16>(x, f);
-    if (!NEAR) {
-      const uint4 y = make_uint4(__shfl(x.x, partner, kWave), __shfl(x.y, partner, kWave), __shfl(x.z, partner, kWave), __shfl(x.w, partner, kWave));
-      cvt8<BF16>(y, g);
-    }
-    if (norm) {
-      float sum = 0.f;
+  for (; head < heads; head += kAhead * per) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += f[i] * f[i];
-      const float inv = rsqrtf(row16_allreduce_sum(sum) * (1.f / kHeadDim) + a.eps);
-      const uint4 mine = is_q ? wq : wk, theirs = is_q ? vq : vk;
-      float w[8];
-      cvt8<BF16>(mine, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] *= inv * w[i];
+    for (int y = 0; y < kAhead; ++y) {
+      const int hd = head + y * per;
+      if (hd >= heads) break;
+      const bool is_q = hd < a.Hq, norm = (is_q ? a.q_weight : a.k_weight) != nullptr;
+      const uint4 raw = x[y];
+      if (hd + kAhead * per < heads) x[y] = *reinterpret_cast<const uint4*>(at(hd + kAhead * per));
+      float f[8], g[8];
+      cvt8<BF16>(raw, f);
       if (!NEAR) {
-        cvt8<BF16>(theirs, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] *= inv * w[i];
+        const uint4 other = make_uint4(__shfl(raw.x, partner, kWave), __shfl(raw.y, partner, kWave), __shfl(raw.z, partner, kWave), __shfl(raw.w, partner, kWave));
+        cvt8<BF16>(other, g);
       }
-    }
-    if (turned) {
-      if constexpr (NEAR) {
+      if (norm) {
+        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float u = f[2 * i], v = f[2 * i + 1];
-          f[2 * i] = u * t[i].x - v * t[i].y;
-          f[2 * i + 1] = u * t[i].y + v * t[i].x;
+        for (int i = 0; i < 8; ++i) sum += f[i] * f[i];
+        const float inv = rsqrtf(row16_allreduce_sum(sum) * (1.f / kHeadDim) + a.eps);
+        const uint4 mine = is_q ? wq : wk, theirs = is_q ? vq : vk;
+        float w[8];
+        cvt8<BF16>(mine, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= inv * w[i];
+        if (!NEAR) {
+          cvt8<BF16>(theirs, w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) g[i] *= inv * w[i];
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = second ? g[i] * t[i].y + f[i] * t[i].x : f[i] * t[i].x - g[i] * t[i].y;
       }
+      if (turned) {
+        if constexpr (NEAR) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float u = f[2 * i], v = f[2 * i + 1];
+            f[2 * i] = u * t[i].x - v * t[i].y;
+            f[2 * i + 1] = u * t[i].y + v * t[i].x;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = second ? g[i] * t[i].y + f[i] * t[i].x : f[i] * t[i].x - g[i] * t[i].y;
+        }
+      }
+      uint16_t* to = is_q ? a.q_out + row * a.q_out_stride + (long long)hd * kHeadDim + j * 8
+                          : a.k_out + row * a.k_out_stride + (long long)(hd - a.Hq) * kHeadDim + j * 8;
+      *reinterpret_cast<uint4*>(to) = make_uint4(pack2<BF16>(f[0], f[1]), pack2<BF16>(f[2], f[3]), pack2<BF16>(f[4], f[5]), pack2<BF16>(f[6], f[7]));
     }
-    uint16_t* to = is_q ? a.q_out + row * a.q_out_stride + (long long)head * kHeadDim + j * 8
-                        : a.k_out + row * a.k_out_stride + (long long)(head - a.Hq) * kHeadDim + j * 8;
-    *reinterpret_cast<uint4*>(to) = make_uint4(pack2<BF16>(f[0], f[1]), pack2<BF16>(f[2], f[3]), pack2<BF16>(f[4], f[5]), pack2<BF16>(f[6], f[7]));
-    x = next;
   }
 }
 
