@@ -49,7 +49,7 @@ struct AttnArgs {
   int32_t* ticket;
   int B, NP, T, H, G, P, NB, R, W, window;
   u32 page_magic;                              // ceil(2^32 / tiles of a page), for pages of several
-  float scale_log2, cap_in, cap_out;           // logits in powers of two: s * scale_log2, or cap_out * tanh(s * cap_in / 2 log2 e)
+  float scale_log2, cap_in, cap_out;           // logits in powers of two: s * scale_log2, or cap_out * tanh(s * cap_in * ln 2 / 2); 0: no cap
 };
 
 template <int N, class F>
@@ -59,7 +59,11 @@ __device__ __forceinline__ void each_of(F f) {
     f(std::integral_constant<int, N - 1>{});
   }
 }
-__device__ __forceinline__ i32x4 load_codes(const unsigned char* p) { return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p)); }
+template <bool ONCE>                           // whether nobody else reads them
+__device__ __forceinline__ i32x4 load_codes(const unsigned char* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p));
+  else return *reinterpret_cast<const i32x4*>(p);
+}
 __device__ __forceinline__ i32x4 load_scales(const unsigned char* p) { return *reinterpret_cast<const i32x4*>(p); }
 __device__ __forceinline__ u64 pack_floats(float a, float b) { return (u64)as_u32(b) << 32 | as_u32(a); }
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
@@ -96,6 +100,12 @@ __device__ __forceinline__ void parts(const float* x, bf16x8 (&to)[NP]) {
   if constexpr (NP > 1) to[1] = __builtin_bit_cast(bf16x8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
 }
 
+// a * b + c of two 16-bit whole numbers each (which the compiler would take apart where b is a power of two)
+__device__ __forceinline__ u16x2 mad_pair(u32 a, u32 b, u32 c) {
+  u32 x;
+  asm("v_pk_mad_u16 %0, %1, %2, %3" : "=v"(x) : "v"(a), "s"(b), "v"(c));
+  return __builtin_bit_cast(u16x2, x);
+}
 // Eight weights, none of them negative, to NP operands whose parts are not negative either: rounded to bf16, or cut, and what that left
 template <int NP>
 __device__ __forceinline__ void weights(const float* p, u16x2 (&to)[NP][4]) {
@@ -117,7 +127,7 @@ struct Seen {
 };
 
 // Sixteen columns: lane (c, n) = (lane / 16, lane % 16) has elements 16 i + 4 c + 0..3 of column n in o[i]
-template <bool BF16, int HEAD>
+template <bool BF16, bool SHAPED, int HEAD>
 struct Columns {
   static constexpr float kHead = HEAD;
   static constexpr int NP = BF16 ? 1 : 2;      // parts of bf16 that a number of q's type has
@@ -169,26 +179,34 @@ struct Columns {
       for (int i = 0; i < 4; ++i) q[i][0] = __builtin_bit_cast(bf16x8, make_uint4(~0u, ~0u, ~0u, ~0u));
     clear();
   }
-  // Products of N x 4 tokens to logits in powers of two, but for the factor that is returned; at(j): the position of the first four of s[j]
+  // Products of N x 4 tokens to logits in powers of two, but for the factor that is returned, and less cap_out; at(j): the position of
+  // the first four of s[j]
   template <int N, class At>
   __device__ __forceinline__ float logits(const AttnArgs& a, f32x4 (&s)[N], At at) const {
     float scale = a.scale_log2;
+    if constexpr (!SHAPED) return scale;
     if (a.cap_in != 0.f) {
-      scale = 1.f;
+      scale = 2.f * a.cap_out;
 #pragma unroll
       for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {          // tanh x = 1 - 2 / (e^2x + 1)
-          const float e = __builtin_amdgcn_exp2f(s[j][i] * a.cap_in);
-          s[j][i] = a.cap_out - 2.f * a.cap_out * __builtin_amdgcn_rcpf(e + 1.f);
-        }
+        for (int i = 0; i < 4; ++i)            // tanh x = 1 - 2 / (e^2x + 1)
+          s[j][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[j][i] * a.cap_in));
     }
     if (a.slopes) {
       const float far = (float)(at(0) - pos);  // (below 2^24: exact, and its sums)
+      if (a.prefix_len) {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[j][i] = s[j][i] * scale - slope * fabsf(far + (float)(at(j) - at(0) + i));
+          for (int i = 0; i < 4; ++i) s[j][i] = __builtin_fmaf(s[j][i], scale, -slope * fabsf(far + (float)(at(j) - at(0) + i)));
+      } else {                                 // what is seen lies before the row
+        const float bias = slope * far;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[j][i] = __builtin_fmaf(s[j][i], scale, __builtin_fmaf(slope, (float)(at(j) - at(0) + i), bias));
+      }
       scale = 1.f;
     }
     return scale;
@@ -276,7 +294,7 @@ __device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, in
   for (int i = 0; i < N / 2; ++i) w[i] = pack2<BF16>(l == 0.f ? 0.f : v[2 * i] * inv, l == 0.f ? 0.f : v[2 * i + 1] * inv);
   if constexpr (N == 8) *reinterpret_cast<uint4*>(a.out + at * kHeadDim + d) = make_uint4(w[0], w[1], w[2], w[3]);
   else *reinterpret_cast<uint2*>(a.out + at * kHeadDim + d) = make_uint2(w[0], w[1]);
-  if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l) + a.cap_out) * kLn2;
 }
 
 // Tiles of a sequence's pages
@@ -301,13 +319,13 @@ __device__ __forceinline__ const unsigned char* tile_at(const AttnArgs& a, u32 l
 // A wave's 128 tokens at a time.  Values' scales are one for 32 elements of a token, which the second product sums over: they go into the
 // weights, so that each group of 32 columns of V has weights of its own, p * 2^e.  Where columns would be empty they repeat the
 // rows (REP): each copy weighs the values of a fraction of the groups.  CG waves share tokens and have 16 columns each.
-template <bool BF16, int REP, int CG>
+template <bool BF16, bool SHAPED, int REP, int CG>
 struct Wave {
-  static constexpr int NP = Columns<BF16, kFewHead>::NP;
+  static constexpr int NP = Columns<BF16, SHAPED, kFewHead>::NP;
   static constexpr int kCols = 16 / REP;       // columns that differ
   static constexpr int kGroups = 4 / REP;      // of V's groups of 32 columns, those that a lane weighs
   static_assert(CG == 1 || REP == 1, "");
-  Columns<BF16, kFewHead> x;
+  Columns<BF16, SHAPED, kFewHead> x;
   Seen seen;
 
   const AttnArgs& a;
@@ -353,7 +371,7 @@ struct Wave {
     for (int half = 0; half < 2; ++half) {
       const unsigned char* at = tile(lines, 2 * (n >> 2) + half) + (n & 3) * 64 + c * 16;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k[half * 4 + j] = load_codes(at + j * 256);
+      for (int j = 0; j < 4; ++j) k[half * 4 + j] = load_codes<CG == 1>(at + j * 256);
       ks[half] = *reinterpret_cast<const u32*>(at - (n & 3) * 60 + kKeyScales);
     }
   }
@@ -361,8 +379,8 @@ struct Wave {
     const unsigned char *at0 = tile(lines, 2 * c), *at1 = tile(lines, 2 * c + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      v[2 * i] = load_codes(at0 + kValues + n * 16 + i * 256);
-      v[2 * i + 1] = load_codes(at1 + kValues + n * 16 + i * 256);
+      v[2 * i] = load_codes<CG == 1>(at0 + kValues + n * 16 + i * 256);
+      v[2 * i + 1] = load_codes<CG == 1>(at1 + kValues + n * 16 + i * 256);
     }
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
@@ -392,6 +410,7 @@ struct Wave {
   // bf16's bits less 126 - e in its exponent, which are those of a smaller number, and 0 where there would be none; p is up to 2^98.
   template <int X>
   __device__ __forceinline__ void weigh(const u16x2 (&p)[4][NP][4]) {
+    const u32 times = 0x10001u * (u32)(0x10000 - 128), most = 0x10001u * ((kBias + kFewDown) << 7);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {              // eight of the lane's tokens
       bf16x8 B[NP];
@@ -399,7 +418,7 @@ struct Wave {
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         const u32 bytes = __builtin_amdgcn_perm(0, (u32)vs[X][i >> 1][(i & 1) * 2 + (y >> 1)], y & 1 ? 0x0c030c02 : 0x0c010c00);
-        const u16x2 down = (unsigned short)((kBias + kFewDown) << 7) - __builtin_bit_cast(u16x2, bytes) * (unsigned short)128;
+        const u16x2 down = mad_pair(bytes, times, most);
 #pragma unroll
         for (int z = 0; z < NP; ++z) w[z][y] = __builtin_elementwise_sub_sat(p[i][z][y], down);
       }
@@ -467,9 +486,9 @@ struct AttnLds {
 };
 
 // The results of the waves that share columns as one: with to_slot < 0 to the output, else there
-template <bool BF16, int REP, int CG>
-__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, REP, CG>& w, AttnLds& lds, int to_slot) {
-  typedef Wave<BF16, REP, CG> W;
+template <bool BF16, bool SHAPED, int REP, int CG>
+__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, SHAPED, REP, CG>& w, AttnLds& lds, int to_slot) {
+  typedef Wave<BF16, SHAPED, REP, CG> W;
   const int tid = threadIdx.x, wave = tid / kWave;
   __syncthreads();                             // (what was there has been read)
   if (w.c == 0) {
@@ -520,8 +539,8 @@ __device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, 
 // Tiles [t0, t1) of a unit: by all waves, or, if they are one step (`step`), by those of turn `solo` alone.  Its result goes to the output if it is
 // all of the unit (count == 1), else to slot `mine` of the partial results, which the last of the `count` pieces to arrive
 // joins, in their order; slot(i) is the i-th one's number.
-template <bool BF16, int REP, int CG, class Slot>
-__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, REP, CG>& w, AttnLds& lds, const Unit& u, int t0, int t1,
+template <bool BF16, bool SHAPED, int REP, int CG, class Slot>
+__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, SHAPED, REP, CG>& w, AttnLds& lds, const Unit& u, int t0, int t1,
                                       bool step, int solo, int count, int mine, int ticket, Slot slot) {
   constexpr int kShares = kAttnWaves / CG;
   const int share = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) / CG;
@@ -575,10 +594,10 @@ __device__ __forceinline__ auto lead_of(const AttnArgs& a) {
   return [&a](int row0) { return a.row_from && row0 < a.T ? max(a.row_from[row0], 0) / kTile : 0; };
 }
 
-template <bool BF16, int REP, int CG>
+template <bool BF16, bool SHAPED, int REP, int CG>
 __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
   __shared__ AttnLds lds;
-  Wave<BF16, REP, CG> w(a);
+  Wave<BF16, SHAPED, REP, CG> w(a);
   int solo = 0;
   deal<kAttnThreads, kLeastTiles, kPieceTiles>(a, false, most_tiles(a), lead_of(a), [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
     const int first = first_tile(a, u);
@@ -601,13 +620,13 @@ struct RowsLds {
   int first[kAttnWaves], behind[kAttnWaves];
 };
 
-template <bool BF16>
+template <bool BF16, bool SHAPED>
 __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs a) {
-  constexpr int NQ = kRowGroups, NP = Columns<BF16, kRowsHead>::NP;
+  constexpr int NQ = kRowGroups, NP = Columns<BF16, SHAPED, kRowsHead>::NP;
   __shared__ RowsLds lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, c = lane >> 4, n = lane & 15;
   const int rows = a.R / kAttnWaves;           // of a wave
-  Columns<BF16, kRowsHead> x[NQ];
+  Columns<BF16, SHAPED, kRowsHead> x[NQ];
   const bool grow = !windowed(a) && a.prefix_len == nullptr;
   deal<kAttnThreads, kLeastTiles, 0>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
@@ -844,16 +863,20 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
   a.R = shape.groups ? 16 * shape.groups / shape.copies / a.G : 16 * kRowGroups / a.G * kAttnWaves;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.W), dim3(kAttnThreads), 0, s, a); };
-  auto typed = [&](auto bf16) {
-    constexpr bool B = decltype(bf16)::value;
-    if (shape.copies == 4) go(q4_attn_kernel<B, 4, 1>);
-    else if (shape.copies == 2) go(q4_attn_kernel<B, 2, 1>);
-    else if (shape.groups == 1) go(q4_attn_kernel<B, 1, 1>);
-    else if (shape.groups == 2) go(q4_attn_kernel<B, 1, 2>);
-    else if (shape.groups == 4) go(q4_attn_kernel<B, 1, 4>);
-    else go(q4_attn_rows_kernel<B>);
+  auto typed = [&](auto bf16, auto shaped) {
+    constexpr bool B = decltype(bf16)::value, S = decltype(shaped)::value;
+    if (shape.copies == 4) go(q4_attn_kernel<B, S, 4, 1>);
+    else if (shape.copies == 2) go(q4_attn_kernel<B, S, 2, 1>);
+    else if (shape.groups == 1) go(q4_attn_kernel<B, S, 1, 1>);
+    else if (shape.groups == 2) go(q4_attn_kernel<B, S, 1, 2>);
+    else if (shape.groups == 4) go(q4_attn_kernel<B, S, 1, 4>);
+    else go(q4_attn_rows_kernel<B, S>);
   };
-  if (c->kv_dtype == KVD_BF16) typed(std::true_type{});
-  else typed(std::false_type{});
+  const bool shaped = a.cap_in != 0.f || a.slopes != nullptr;
+  if (c->kv_dtype == KVD_BF16) {
+    if (shaped) typed(std::true_type{}, std::true_type{}); else typed(std::true_type{}, std::false_type{});
+  } else {
+    if (shaped) typed(std::false_type{}, std::true_type{}); else typed(std::false_type{}, std::false_type{});
+  }
   return launched();
 }
