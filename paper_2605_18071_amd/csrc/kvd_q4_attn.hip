@@ -29,6 +29,7 @@ constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnGroups = 512;               // workgroups: two for each CU
 constexpr int kStep = 8;                       // tiles that a wave takes at a time
 constexpr int kLeastTiles = 32;                // tiles of a workgroup at least
+constexpr int kFewPad = 16, kRowsPad = 24;     // what a unit costs whatever its length: tiles
 constexpr int kPieceTiles = 64;                // tiles of a workgroup where there are few
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 constexpr int kPartWords = 16 * kWave + 16;    // 8-byte words of 16 columns' partial result: accumulators, then a maximum and a sum a column
@@ -599,7 +600,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
   __shared__ AttnLds lds;
   Wave<BF16, SHAPED, REP, CG> w(a);
   int solo = 0;
-  deal<kAttnThreads, kLeastTiles, kPieceTiles>(a, false, most_tiles(a), lead_of(a), [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<kAttnThreads, kLeastTiles, kPieceTiles, kFewPad>(a, false, most_tiles(a), lead_of(a), [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
     const int first = first_tile(a, u);
     piece(a, w, lds, u, t0 > 0 ? first + t0 : 0, first + t1, t1 - t0 <= kStep, solo, count, mine, f, slot);
     ++solo;
@@ -608,27 +609,30 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
 
 // ---- many rows
 
-// Each wave has its own kRowGroups * 16 columns, and the workgroup goes through the tokens together, 64 at a time: every wave fetches one
-// tile, widens it and puts it into LDS in operand order, while the 64 before it are taken; so a code is widened once for four
-// waves.  Values take their scales there.
+// Each wave has its own kRowGroups * 16 columns, and the workgroup's WAVES go through the tokens together, 64 at a time: waves fetch a
+// tile each, widen it and put it into LDS in operand order, while the 64 before it are taken; so a code is widened once for all
+// of them.  Values take their scales there.  Of eight waves four have the keys and four the values.
 constexpr int kRowGroups = 2;
-constexpr int kStageTiles = kAttnWaves;
+constexpr int kStageTiles = 4;
+template <int WAVES>
 struct RowsLds {
   uint4 k[2][kStageTiles][4][kWave];           // [stage][tile][8 elements of 32][lane]
   uint4 v[2][kStageTiles / 2][8][kWave];       // [stage][pair of tiles][16 elements][lane]
   u32 line[2][kStageTiles];
-  int first[kAttnWaves], behind[kAttnWaves];
+  int first[WAVES], behind[WAVES];
 };
 
-template <bool BF16, bool SHAPED>
-__global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs a) {
+template <bool BF16, bool SHAPED, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs a) {
   constexpr int NQ = kRowGroups, NP = Columns<BF16, SHAPED, kRowsHead>::NP;
-  __shared__ RowsLds lds;
+  __shared__ RowsLds<WAVES> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, c = lane >> 4, n = lane & 15;
-  const int rows = a.R / kAttnWaves;           // of a wave
+  const int rows = a.R / WAVES;                // of a wave
+  const int tile = wave % kStageTiles;         // of a stage, the one that this wave fetches
+  const bool keys = wave < kStageTiles, values = WAVES == kStageTiles || !keys;
   Columns<BF16, SHAPED, kRowsHead> x[NQ];
   const bool grow = !windowed(a) && a.prefix_len == nullptr;
-  deal<kAttnThreads, kLeastTiles, 0>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<WAVES * kWave, kLeastTiles, 0, kRowsPad>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
     u.row0 += wave * rows;
     u.pos0 += wave * rows;
@@ -649,28 +653,36 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
     const int first = first_tile(a, whole);
     int from = lds.first[0], to = lds.behind[0];
 #pragma unroll
-    for (int i = 1; i < kAttnWaves; ++i) { from = min(from, lds.first[i]); to = max(to, lds.behind[i]); }
+    for (int i = 1; i < WAVES; ++i) { from = min(from, lds.first[i]); to = max(to, lds.behind[i]); }
     from = __builtin_amdgcn_readfirstlane(max(t0 > 0 ? first + t0 : 0, from));
     to = __builtin_amdgcn_readfirstlane(min(first + t1, to));
 
-    i32x4 kc, vc, vsc;                         // this wave's tile on its way: codes of keys and values, scales of values
+    i32x4 kc = {}, vc = {}, vsc = {};          // this wave's tile on its way: codes of keys and values, scales of values
     u32 ksc = 0, line = kNoTile;
     int block = -1;
     auto fetch = [&](int t) {                  // tile t, whose block is at hand, and the block of the one after it
       line = tiles.line(t, to, block);
       block = tiles.block(min(t + kStageTiles, to - 1));
       const unsigned char* at = tile_at(a, line);
-      kc = load_scales(at + n * 64 + c * 16);
-      vc = load_scales(at + kValues + lane * 16);
-      vsc = load_scales(at + kValueScales + c * 16);
-      ksc = at[kKeyScales + c * 16 + (n & 3) * 4 + (n >> 2)];
+      if (keys) {
+        kc = load_scales(at + n * 64 + c * 16);
+        ksc = at[kKeyScales + c * 16 + (n & 3) * 4 + (n >> 2)];
+      }
+      if (values) {
+        vc = load_scales(at + kValues + lane * 16);
+        vsc = load_scales(at + kValueScales + c * 16);
+      }
     };
     auto put = [&](int s) {
-      const float scale = two_to((int)ksc - kBias);
+      if (keys) {
+        const float scale = two_to((int)ksc - kBias);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) lds.k[s][wave][i][lane] = __builtin_bit_cast(uint4, widen(kc[i], scale));
+        for (int i = 0; i < 4; ++i) lds.k[s][tile][i][lane] = __builtin_bit_cast(uint4, widen(kc[i], scale));
+        if (lane == 0) lds.line[s][tile] = line;
+      }
+      if (!values) return;
       // lane l has elements 32 (l / 16) + l % 16 and 16 more, 16 tokens each: two tokens of a byte, a scale each
-      u64* to_v = reinterpret_cast<u64*>(&lds.v[s][wave >> 1][2 * c][n]) + (wave & 1);
+      u64* to_v = reinterpret_cast<u64*>(&lds.v[s][tile >> 1][2 * c][n]) + (tile & 1);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {            // tokens 4 i + 0..3, which are lane (i, n)'s
         float e[4];
@@ -692,16 +704,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
           to_v[(half * kWave + i * 16) * 2] = (u64)two[1] << 32 | two[0];
         }
       }
-      if (lane == 0) lds.line[s][wave] = line;
     };
     if (from < to) {
-      block = tiles.block(min(from + wave, to - 1));
-      fetch(from + wave);
+      block = tiles.block(min(from + tile, to - 1));
+      fetch(from + tile);
       put(0);
       __syncthreads();
       int stage = 0;
       for (int t = from; t < to; t += kStageTiles, stage ^= 1) {
-        fetch(t + kStageTiles + wave);
+        fetch(t + kStageTiles + tile);
         if (t < seen.behind && t + kStageTiles > seen.first) {
           // operands are asked for four at a time, while the four before them are taken: keys of two tiles, two of their four
           // parts each, then values of a pair of tiles, four of their eight
@@ -766,7 +777,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
 #pragma unroll
     for (int g = 0; g < NQ; ++g) x[g].l = sum_of_column(x[g].l);
     if (count > 1) {
-      auto part_of = [&](int i, int g) { return a.part + (((size_t)i * kAttnWaves + wave) * NQ + g) * kPartWords; };
+      auto part_of = [&](int i, int g) { return a.part + (((size_t)i * WAVES + wave) * NQ + g) * kPartWords; };
 #pragma unroll
       for (int g = 0; g < NQ; ++g) {
         u64* part = part_of(mine, g);
@@ -779,10 +790,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
       }
       wave_drain_memory();                     // (written through and drained before the ticket, and read past the caches)
       int before = 0;
-      if (lane == 0) before = __hip_atomic_fetch_add(a.ticket + f * kAttnWaves + wave, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (lane == 0) before = __hip_atomic_fetch_add(a.ticket + f * WAVES + wave, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       last = __builtin_amdgcn_readfirstlane(before) == count - 1;
       if (last) {
-        if (lane == 0) store_agent(a.ticket + f * kAttnWaves + wave, 0);
+        if (lane == 0) store_agent(a.ticket + f * WAVES + wave, 0);
 #pragma unroll
         for (int g = 0; g < NQ; ++g) x[g].clear();
         for (int i = 0; i < count; ++i)
@@ -805,11 +816,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_rows_kernel(AttnArgs 
 }
 
 // How the columns that the rows of a sequence take, on the average, are laid out: copies of them in 16, or groups of 16 (0: waves with
-// rows of their own)
-struct Shape { int copies, groups; };
+// rows of their own, of 4 or 8 waves)
+struct Shape { int copies, groups, waves; };
 static Shape shape_of(int T, int B, int G) {
   const int64_t want = (int64_t)((T + B - 1) / B) * G;
-  return {want <= 4 ? 4 : want <= 8 ? 2 : 1, want <= 16 ? 1 : want <= 32 ? 2 : want <= 64 ? 4 : 0};
+  return {want <= 4 ? 4 : want <= 8 ? 2 : 1, want <= 16 ? 1 : want <= 32 ? 2 : want <= 64 ? 4 : 0, want <= 128 ? 4 : 8};
 }
 
 }  // namespace q4
@@ -820,7 +831,7 @@ extern "C" int64_t kvd_q4_workspace_bytes(const kvd_q4_cache* c, const kvd_q8_ro
   if (int e = check_cache(c, r)) return e;
   static_assert(kAttnGroups * kAttnWaves * 4 <= kvd::q8::kTicketBytes, "a ticket for each wave of each workgroup");
   const Shape shape = shape_of(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
-  return kvd::q8::kTicketBytes + (int64_t)kAttnGroups * 2 * 8 * kPartWords * (shape.groups ? shape.groups : kAttnWaves * kRowGroups);
+  return kvd::q8::kTicketBytes + (int64_t)kAttnGroups * 2 * 8 * kPartWords * (shape.groups ? shape.groups : kAttnWaves * kRowGroups);  // (8 waves: half as many workgroups)
 }
 
 extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const void* q, int64_t q_stride, const kvd_q4_scores* f,
@@ -856,13 +867,13 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
   a.part = reinterpret_cast<kvd::u64*>(static_cast<char*>(workspace) + kvd::q8::kTicketBytes);
   a.B = r->n_seqs; a.NP = r->max_pages; a.T = r->n_rows; a.H = c->n_kv_heads; a.G = c->n_q_heads / c->n_kv_heads;
   a.P = c->page_size; a.NB = c->n_blocks;
-  a.W = kAttnGroups;
   const int tpp = a.P / kTile;
   a.page_magic = (kvd::u32)(((1ull << 32) + tpp - 1) / tpp);
   const Shape shape = shape_of(a.T, a.B, a.G);
-  a.R = shape.groups ? 16 * shape.groups / shape.copies / a.G : 16 * kRowGroups / a.G * kAttnWaves;
+  a.R = shape.groups ? 16 * shape.groups / shape.copies / a.G : 16 * kRowGroups / a.G * shape.waves;
+  a.W = shape.groups || shape.waves == kAttnWaves ? kAttnGroups : kAttnGroups / 2;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.W), dim3(kAttnThreads), 0, s, a); };
+  auto go = [&](auto kernel, int waves = kAttnWaves) { hipLaunchKernelGGL(kernel, dim3(a.W), dim3(waves * kvd::kWave), 0, s, a); };
   auto typed = [&](auto bf16, auto shaped) {
     constexpr bool B = decltype(bf16)::value, S = decltype(shaped)::value;
     if (shape.copies == 4) go(q4_attn_kernel<B, S, 4, 1>);
@@ -870,7 +881,8 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
     else if (shape.groups == 1) go(q4_attn_kernel<B, S, 1, 1>);
     else if (shape.groups == 2) go(q4_attn_kernel<B, S, 1, 2>);
     else if (shape.groups == 4) go(q4_attn_kernel<B, S, 1, 4>);
-    else go(q4_attn_rows_kernel<B, S>);
+    else if (shape.waves == 4) go(q4_attn_rows_kernel<B, S, 4>);
+    else go(q4_attn_rows_kernel<B, S, 8>, 8);
   };
   const bool shaped = a.cap_in != 0.f || a.slopes != nullptr;
   if (c->kv_dtype == KVD_BF16) {

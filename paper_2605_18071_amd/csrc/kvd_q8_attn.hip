@@ -556,7 +556,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_dense_kernel(AttnArgs
   __shared__ AttnLds<NQ> lds;
   Wave<BF16, NQ, DUP, !DUP, false> w(a);
   int solo = 0;
-  deal<kAttnThreads, kLeastTiles, 0>(a, false, kAllTiles, [](int) { return 0; }, [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<kAttnThreads, kLeastTiles, 0, 0>(a, false, kAllTiles, [](int) { return 0; }, [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
     piece(a, w, lds, u, t0, t1, solo, count, mine, f, slot);
     solo = (solo + 1) % kAttnWaves;
   });
@@ -583,7 +583,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q8_attn_rows_kernel(AttnArgs 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Wave<BF16, NQ, false, !BF16, false> w(a);
   const int tpp = a.P / kTile, rows = a.R / kAttnWaves;                // tiles of a page; rows of a wave
-  deal<kAttnThreads, kLeastTiles, 0>(a, true, kAllTiles, [](int) { return 0; }, [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<kAttnThreads, kLeastTiles, 0, 0>(a, true, kAllTiles, [](int) { return 0; }, [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
     u.row0 += wave * rows;
     u.pos0 += wave * rows;

@@ -25,15 +25,16 @@ __device__ __forceinline__ u64 uniform(u64 x) {
 // `most` bounds the tiles of a unit; a.W workgroups (a multiple of kXcds) have LEAST tiles at least.  ALIGN > 0: if the units are few
 // enough for a workgroup to each ALIGN tiles of one, that is how they are dealt out (not where they grow): then a unit of no more than
 // that needs no joining, which takes longer than its tiles.  lead(row): tiles at the beginning of the sequence that begins with that
-// row which are left out of the count.
-template <int NT, int LEAST, int ALIGN, class Args, class Lead, class Each>
+// row which are left out of the count.  PAD (less than LEAST): what a unit costs
+// whatever its length, in tiles, which it counts for at its beginning; a share that would begin in there begins with the unit.
+template <int NT, int LEAST, int ALIGN, int PAD, class Args, class Lead, class Each>
 __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Lead lead, Each each) {
   __shared__ u64 scan[NT / kWave];
   __shared__ u64 s_base;
   __shared__ int s_seq;
   const int tid = threadIdx.x, lane = tid % kWave, wv = tid / kWave;
   const int more = grow ? (a.R + kTile - 1) / kTile : 0;
-  int align = 1;                               // what a unit's tiles are rounded up to
+  int align = 1, pad = PAD;                    // what a unit's tiles are rounded up to, and what they are preceded by
   int skip = 0;                                // lead of the sequence that was last asked for
   auto of = [&](int b, int& row0, int& rows, int& len, int& first) {   // returns units a head
     row0 = min(max(a.row_start[b], 0), a.T);
@@ -41,7 +42,7 @@ __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Lead le
     len = min(max(a.kv_len[b], 0), a.NP * a.P);
     first = max(((grow ? min(len, max(len - rows, 0) + a.R) : len) + kTile - 1) / kTile, 1);
     skip = rows > 0 ? min(lead(row0), first - 1) : 0;
-    first = min(first - skip, most);
+    first = min(first - skip, most) + pad;
     if (ALIGN > 0) first = (first + align - 1) / align * align;
     return (rows + a.R - 1) / a.R;
   };
@@ -72,9 +73,11 @@ __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Lead le
   };
   if (ALIGN > 0 && !grow) {
     align = ALIGN;
+    pad = 0;
     count();
     if (all > (u64)a.W * ALIGN) {
       align = 1;
+      pad = PAD;
       __syncthreads();                         // (the sums have been read)
       count();
     }
@@ -127,7 +130,18 @@ __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Lead le
         part = uniform(part);
       }
       const u64 begin = base + h * of_head + upto_unit(part, first);
-      const int tiles = first + (int)part * more, t0 = (int)(at - begin), t1 = (int)min((u64)tiles, stop - begin);
+      const int tiles = first + (int)part * more;
+      int t0 = (int)(at - begin), t1 = (int)min((u64)tiles, stop - begin), f = (int)(begin / per_group);
+      const int last = (int)((begin + tiles - 1) / per_group);
+      at = begin + t1;
+      if (PAD > 0 && pad > 0) {
+        static_assert(PAD < LEAST, "");
+        if (t1 <= pad && t1 < tiles) break;    // (the next workgroup begins with the unit)
+        f = (int)((begin + pad) / per_group);
+        t0 = max(t0 - pad, 0);
+        t1 -= pad;
+      }
+      const int count = last - f + 1;
       Unit u;
       u.lead = in_front;
       u.seq = b;
@@ -136,10 +150,8 @@ __device__ __forceinline__ void deal(const Args& a, bool grow, int most, Lead le
       u.rows = min(a.R, rows - (int)part * a.R);
       u.pos0 = len - rows + (int)part * a.R;
       u.entries = min((len + a.P - 1) / a.P, a.NP);
-      const int f = (int)(begin / per_group), count = (int)((begin + tiles - 1) / per_group) - f + 1;
       // a workgroup has the beginning of one unit that goes on behind it, and at most one piece that began before it
       each(u, t0, t1, f, count, group * 2 + (t0 == 0 ? 1 : 0), [f](int x) { return x == 0 ? f * 2 + 1 : (f + x) * 2; });
-      at = begin + t1;
     }
     base = end;
     ++b;

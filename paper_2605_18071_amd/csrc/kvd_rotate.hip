@@ -43,7 +43,8 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_kernel(RotateArgs a) 
   const long long row = row0 + group % NR;
   const int heads = a.Hq + a.Hk, per = kGroups / NR * gridDim.y;
   int head = blockIdx.y * (kGroups / NR) + group / NR;
-  const bool real = row < a.T && a.pos[row] >= 0;
+  // everything is asked for at the beginning, whether the row has a token or not
+  const int place = row < a.T ? a.pos[row] : -1;
   auto at = [&](int h) {
     return h < a.Hq ? a.q + row * a.q_stride + (long long)h * kHeadDim + j * 8
                     : a.k + row * a.k_stride + (long long)(h - a.Hq) * kHeadDim + j * 8;
@@ -52,24 +53,10 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_kernel(RotateArgs a) 
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) {
     x[i] = make_uint4(0, 0, 0, 0);
-    if (real && head + i * per < heads) x[i] = *reinterpret_cast<const uint4*>(at(head + i * per));
+    if (row < a.T && head + i * per < heads) x[i] = *reinterpret_cast<const uint4*>(at(head + i * per));
   }
-  for (int i = tid; i < NR * kMaxPairs; i += kRotThreads) {
-    const int r = i / kMaxPairs, p = i % kMaxPairs;
-    if (p < a.pairs && row0 + r < a.T) {
-      const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
-      const double turns = (double)a.pos[axis * a.pos_stride + row0 + r] * ((double)a.inv_freq[p] * 0.15915494309189533577);
-      turn[r][p] = cos_sin((float)(turns - rint(turns)));
-    }
-  }
-  __syncthreads();
-  // the lane's cosines and sines: of its four pairs, or of the eight that its elements are one half of
   const int half = a.pairs / 8;                // lanes of the first elements of pairs that lie apart
   const bool turned = NEAR ? j < 2 * half : j < 2 * half, second = !NEAR && j >= half;
-  float2 t[NEAR ? 4 : 8];
-  if (turned)
-#pragma unroll
-    for (int i = 0; i < (NEAR ? 4 : 8); ++i) t[i] = turn[group % NR][NEAR ? j * 4 + i : (second ? j - half : j) * 8 + i];
   const int lane = tid % kWave, partner = (lane & ~15) + (turned ? (second ? j - half : j + half) : j);
   // weights: of the lane's elements and of its partner's, of both kinds of heads
   uint4 wq = make_uint4(0, 0, 0, 0), wk = wq, vq = wq, vk = wq;
@@ -81,7 +68,21 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_kernel(RotateArgs a) 
     wk = *reinterpret_cast<const uint4*>(a.k_weight + j * 8);
     vk = *reinterpret_cast<const uint4*>(a.k_weight + (partner & 15) * 8);
   }
-  if (!real) return;                           // (whole groups of 16 lanes)
+  for (int i = tid; i < NR * kMaxPairs; i += kRotThreads) {
+    const int r = i / kMaxPairs, p = i % kMaxPairs;
+    if (p < a.pairs && row0 + r < a.T) {
+      const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
+      const double turns = (double)a.pos[axis * a.pos_stride + row0 + r] * ((double)a.inv_freq[p] * 0.15915494309189533577);
+      turn[r][p] = cos_sin((float)(turns - rint(turns)));
+    }
+  }
+  __syncthreads();
+  // the lane's cosines and sines: of its four pairs, or of the eight that its elements are one half of
+  float2 t[NEAR ? 4 : 8];
+  if (turned)
+#pragma unroll
+    for (int i = 0; i < (NEAR ? 4 : 8); ++i) t[i] = turn[group % NR][NEAR ? j * 4 + i : (second ? j - half : j) * 8 + i];
+  if (place < 0) return;                       // (whole groups of 16 lanes)
   for (; head < heads; head += kAhead * per) {
 #pragma unroll
     for (int y = 0; y < kAhead; ++y) {

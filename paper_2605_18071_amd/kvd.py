@@ -629,17 +629,23 @@ class Q8Rows(_OnDevice):
                    free_blocks.numel(), free_count.data_ptr())
 
 
+def _ordinal(device: torch.device) -> int:
+    """A device as Tensor.get_device() has it, which is quicker to compare."""
+    return device.index if device.type == "cuda" else -1
+
+
 class _Heads(_OnDevice):
     """What has tensors of [rows][heads][head_dim]."""
 
     def _rowed(self, name: str, t: torch.Tensor, heads: int, n_rows: int) -> int:
         """Stride of a [rows][heads][head_dim] tensor whose rows may lie apart."""
         D = self.head_dim
-        row, head, element = t.stride() if t.dim() == 3 else (0, 0, 0)
-        if t.shape != (n_rows, heads, D) or t.dtype is not self.kv_dtype or t.device != self.device or head != D or element != 1:
-            raise ValueError(f"{name}: a {self.kv_dtype} tensor of {(n_rows, heads, D)} on {self.device} with whole rows is wanted, "
-                             f"got {t.dtype} of {tuple(t.shape)}, strides {t.stride()} on {t.device}")
-        return row if n_rows > 1 else heads * D
+        if t.shape == (n_rows, heads, D) and t.dtype is self.kv_dtype and t.get_device() == self.ordinal:
+            row, head, element = t.stride()
+            if head == D and element == 1:
+                return row if n_rows > 1 else heads * D
+        raise ValueError(f"{name}: a {self.kv_dtype} tensor of {(n_rows, heads, D)} on {self.device} with whole rows is wanted, "
+                         f"got {t.dtype} of {tuple(t.shape)}, strides {t.stride()} on {t.device}")
 
     def _check_rows(self, rows: Q8Rows, workspace: Optional[torch.Tensor] = None):
         if rows.device != self.device:
@@ -664,6 +670,7 @@ class Q8Cache(_Heads):
         buffers = dict(buffers or {})
         _need(not set(buffers) - {"pages", "exps", "means", "mean_scales"}, "buffers: pages, exps, means and mean_scales are wanted")
         self.device = next(iter(buffers.values())).device if buffers else _cuda(device)
+        self.ordinal = _ordinal(self.device)
         _need(page_size >= 16 and page_size % 16 == 0, "page_size: a multiple of 16 is wanted")
         self.kv_dtype = _kv_type(kv_dtype)
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
@@ -729,6 +736,7 @@ class Rotary(_Heads):
                  k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
         self.lib = load()
         self.device = inv_freq.device
+        self.ordinal = _ordinal(self.device)
         self.kv_dtype = _kv_type(kv_dtype)
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         pairs = inv_freq.numel()
@@ -753,14 +761,18 @@ class Rotary(_Heads):
         n_rows = positions.shape[-1]
         shape = (n_rows,) if self.n_axes == 1 and positions.dim() == 1 else (self.n_axes, n_rows)
         _buffer("positions", positions, shape, torch.int32, self.device)
-        _need(q is not None or k is not None, "q or k is wanted")
-        args = []
-        for name, x, out, heads in (("q", q, q_out, self.n_q_heads), ("k", k, k_out, self.n_kv_heads)):
-            _need(x is not None or out is None, f"{name}_out: there is no {name}")
-            out = x if out is None else out
-            args += [_ptr(x), 0 if x is None else self._rowed(name, x, heads, n_rows),
-                     _ptr(out), 0 if out is None else self._rowed(name + "_out", out, heads, n_rows)]
-        self._call("kvd_norm_rotate", stream, self._ref, positions.data_ptr(), n_rows, n_rows, *args)
+        qp, qs, qop, qos = self._heads_of("q", q, "q_out", q_out, self.n_q_heads, n_rows)
+        kp, ks, kop, kos = self._heads_of("k", k, "k_out", k_out, self.n_kv_heads, n_rows)
+        _need(qp is not None or kp is not None, "q or k is wanted")
+        self._call("kvd_norm_rotate", stream, self._ref, positions.data_ptr(), n_rows, n_rows, qp, qs, qop, qos, kp, ks, kop, kos)
+
+    def _heads_of(self, name, x, out_name, out, heads, n_rows):
+        """Pointer and stride of a tensor and of where it goes, which is itself if nothing is given."""
+        if x is None:
+            _need(out is None, out_name + ": there is nothing to write")
+            return None, 0, None, 0
+        stride, p = self._rowed(name, x, heads, n_rows), x.data_ptr()
+        return (p, stride, p, stride) if out is None else (p, stride, out.data_ptr(), self._rowed(out_name, out, heads, n_rows))
 
 
 # ---- paged cache in 4 bits
@@ -773,6 +785,7 @@ class Q4Cache(_Heads):
                  softmax_scale: float = 0.0, device="cuda", pages: Optional[torch.Tensor] = None):
         self.lib = load()
         self.device = pages.device if pages is not None else _cuda(device)
+        self.ordinal = _ordinal(self.device)
         _need(page_size >= 16 and page_size % 16 == 0, "page_size: a multiple of 16 is wanted")
         self.kv_dtype = _kv_type(kv_dtype)
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim

@@ -169,6 +169,36 @@ def test_attend_long_and_ragged(dtype):
     s.check(q, *s.attend(q))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("Gq", [1, 2, 3, 5, 6, 8])
+@pytest.mark.parametrize("lens,news", [([0, 37, 5], [290, 41, 1]), ([9000], [70]), ([3000, 0], [33, 30])])
+def test_attend_many_rows_of_any_group(dtype, Gq, lens, news):
+    s = Step(lens, news, P=32, H=2, G=Gq, dtype=dtype, seed=Gq, spare=1)
+    q = s.query(2.0)
+    s.check(q, *s.attend(q), rows=sorted(set(list(range(0, s.real, 23)) + [s.real - 2, s.real - 1])))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attend_shares_of_units_of_any_length(seed):
+    """Lengths, rows and masks by chance: units that are dealt out whole, in pieces and many to a workgroup, every few rows checked."""
+    rng = np.random.default_rng(seed)
+    B = int(rng.choice([1, 2, 5, 40]))
+    top = {1: 40000, 2: 9000, 5: 5000, 40: 700}[B]
+    lens = np.exp(rng.uniform(0, np.log(top), B)).astype(int).tolist()
+    most = int(rng.choice([1, 2, 6, 40, 300])) if B < 40 else int(rng.choice([1, 3]))
+    news = rng.integers(1, most + 1, B).tolist()
+    s = Step(lens, news, P=int(rng.choice([16, 48, 128])), H=int(rng.choice([1, 3])), G=int(rng.choice([1, 4, 7])), seed=seed, dtype=["bf16", "f16"][seed % 2])
+    q = s.query(2.0)
+    kw = {}
+    if seed % 3 == 1:
+        kw["window"] = int(rng.integers(1, 2000))
+    if seed % 3 == 2:
+        kw["row_from"] = np.array([int(rng.integers(0, p + 2)) for p in s.pos], dtype=np.int32)      # no order among a sequence's rows
+    if seed % 4 == 3:
+        kw["prefix_len"] = rng.integers(0, top, B).astype(np.int32)
+    s.check(q, *s.attend(q, **kw), rows=sorted(set(rng.integers(0, s.real, 24).tolist())), **kw)
+
+
 def test_attend_many_short_sequences():
     rng = np.random.default_rng(5)
     lens = rng.integers(0, 60, 700).tolist()
