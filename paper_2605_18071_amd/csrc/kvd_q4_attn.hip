@@ -351,7 +351,7 @@ struct Wave {
   __device__ __forceinline__ void begin(const Unit& unit) {
     u = unit;
     const int len = min(max(a.kv_len[u.seq], 0), a.NP * a.P);
-    const int prefix = a.prefix_len ? min(a.prefix_len[u.seq], len) : 0;
+    const int prefix = a.prefix_len ? min(max(a.prefix_len[u.seq], 0), len) : 0;
     int see[4] = {0x7fffffff, -1, 0, 0x7fffffff}, r, head;
     const bool ok = column(cg * 16 + n % kCols, r, head);
     x.begin(a, u, ok, r, head, len, prefix, see);
@@ -639,7 +639,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
     u.rows = min(max(whole.rows - wave * rows, 0), rows);
     const Tiles tiles(a, whole);
     const int len = min(max(a.kv_len[u.seq], 0), a.NP * a.P);
-    const int prefix = a.prefix_len ? min(a.prefix_len[u.seq], len) : 0;
+    const int prefix = a.prefix_len ? min(max(a.prefix_len[u.seq], 0), len) : 0;
     int see[4] = {0x7fffffff, -1, 0, 0x7fffffff};
 #pragma unroll
     for (int g = 0; g < NQ; ++g) {

@@ -830,6 +830,7 @@ class Q4Cache(_Heads):
                                   ("prefix_len", prefix_len, rows.n_seqs, torch.int32)):
             if t is not None:
                 _buffer(name, t, (n,), dtype, self.device)
+        _need(0 <= window < 1 << 31, "window: a number of tokens below 2^31 is wanted")
         scores = KvdQ4Scores(softcap, window, _ptr(slopes), _ptr(row_from), _ptr(prefix_len))
         self._call("kvd_q4_attn", stream, self._ref, rows._ref, q.data_ptr(), qs, C.byref(scores), out.data_ptr(), _ptr(lse),
                    workspace.data_ptr(), workspace.nbytes)

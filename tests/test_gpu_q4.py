@@ -213,7 +213,7 @@ def test_attend_many_short_sequences():
 SCORES = [
     dict(softcap=30.0), dict(softcap=0.5), dict(softcap=1000.0), dict(slopes=True), dict(softcap=20.0, slopes=True), dict(window=1),
     dict(window=17), dict(window=300, softcap=30.0), dict(window=10 ** 9), dict(docs=50), dict(docs=1), dict(docs=333, window=100, slopes=True),
-    dict(prefix=[100, 3, 10 ** 6]), dict(prefix=[0, 40, -5], window=30), dict(prefix=[2 ** 31 - 1] * 3, docs=90, slopes=True, softcap=9.0),
+    dict(prefix=[100, 3, 10 ** 6]), dict(prefix=[-2 ** 31, 40, -5], window=30), dict(prefix=[2 ** 31 - 1] * 3, docs=90, slopes=True, softcap=9.0),
 ]
 
 

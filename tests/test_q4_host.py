@@ -126,6 +126,8 @@ def test_the_binding_refuses_before_the_library():
         ("slopes", lambda: cache.attend(rows, q, q.clone(), ws, slopes=torch.zeros(2))),
         ("row_from", lambda: cache.attend(rows, q, q.clone(), ws, row_from=torch.zeros(4))),
         ("prefix_len", lambda: cache.attend(rows, q, q.clone(), ws, prefix_len=torch.zeros(4, dtype=torch.int32))),
+        ("window", lambda: cache.attend(rows, q, q.clone(), ws, window=1 << 31)),
+        ("window", lambda: cache.attend(rows, q, q.clone(), ws, window=-1)),
         ("pages", lambda: kvd.Q4Cache(n_blocks=9, n_q_heads=8, n_kv_heads=2, page_size=16, kv_dtype=torch.bfloat16, pages=cache.pages)),
         ("page_size", lambda: kvd.Q4Cache(n_blocks=9, n_q_heads=8, n_kv_heads=2, page_size=24, kv_dtype=torch.bfloat16, device="cpu")),
         ("kv_dtype", lambda: kvd.Q4Cache(n_blocks=9, n_q_heads=8, n_kv_heads=2, page_size=16, kv_dtype=torch.float32, device="cpu")),
