@@ -11,8 +11,9 @@
 // One pass with a running reference m and sum l of a column: p = 2^(x - m).  m is HEAD above the largest logit when it is set, and
 // is raised only when a logit passes that by more than kSlack, so that the accumulators are rarely touched.  What multiplies values
 // of up to 2^128 stays below 2^-28, so that 2^24 of them have finite sums.
-// bf16: weights are rounded to bf16, by 2^-8 of themselves at most, like their output.  f16, whose outputs would show it: a
-// second product takes what the rounding left (2^-16), and the first one has the queries in two parts of bf16 too.
+// bf16: weights are rounded to bf16, by 2^-8 of themselves at most, like their output (16 bits would cost 4 % at 16 x 32768 tokens and 8 %
+// where contexts are short).  f16, whose outputs would show it: a second product takes what the rounding left (2^-16), and the
+// first one has the queries in two parts of bf16 too.
 #include "kvd_q4.h"
 #include "kvd_q8_deal.h"
 
@@ -29,8 +30,12 @@ constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnGroups = 512;               // workgroups: two for each CU
 constexpr int kStep = 8;                       // tiles that a wave takes at a time
 constexpr int kLeastTiles = 32;                // tiles of a workgroup at least
-constexpr int kFewPad = 16, kRowsPad = 24;     // what a unit costs whatever its length: tiles
-constexpr int kPieceTiles = 64;                // tiles of a workgroup where there are few
+// What a unit costs whatever its length, in tiles: without it the workgroups that have many short units come last (2 x 4096 rows from
+// the start 433 us for 343, 24 drafts of ragged contexts 137 for 131)
+constexpr int kFewPad = 16, kRowsPad = 24;
+// Tiles of a workgroup where there are few, so that most units need no joining: 30 x 3000 tokens of 8 heads 20 us; with 32 26, with 128
+// 25.  4 x 2500: 13.3, 12.8, 16.0
+constexpr int kPieceTiles = 64;
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 constexpr int kPartWords = 16 * kWave + 16;    // 8-byte words of 16 columns' partial result: accumulators, then a maximum and a sum a column
 constexpr float kLowest = -3.0e38f, kSlack = 8.f;
@@ -87,6 +92,13 @@ __device__ __forceinline__ bf16x8 widen(int codes, float scale) {
                              __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
                              __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3)));
   return __builtin_bit_cast(bf16x8, x);
+}
+// The two codes of byte BYTE, times a scale each
+template <int BYTE>
+__device__ __forceinline__ u32 pair(u32 codes, float first, float second) {
+  const u32 lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, first, BYTE));
+  const u32 hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, second, BYTE));
+  return (lo & 0xffffu) | (hi & 0xffff0000u);
 }
 // Eight numbers to NP operands: rounded to bf16, and what that left
 template <int NP>
@@ -317,9 +329,14 @@ __device__ __forceinline__ const unsigned char* tile_at(const AttnArgs& a, u32 l
 
 // ---- few rows
 
-// A wave's 128 tokens at a time.  Values' scales are one for 32 elements of a token, which the second product sums over: they go into the
-// weights, so that each group of 32 columns of V has weights of its own, p * 2^e.  Where columns would be empty they repeat the
-// rows (REP): each copy weighs the values of a fraction of the groups.  CG waves share tokens and have 16 columns each.
+// A wave's 128 tokens at a time, keys and values of the next on their way.  Values' scales are one for 32 elements of a token, which the
+// second product sums over: they go into the weights, so that each group of 32 columns of V has weights of its own, p * 2^e.  Where
+// columns would be empty they repeat the rows (REP): each copy weighs the values of a fraction of the groups.  CG waves share tokens
+// and have 16 columns each.
+// One row a sequence is bound by the memory: 16 x 32768 tokens of 8 heads 99 us (5.8 TB/s); 4 x 1000 tokens 10.9 us by its chain of trips
+// to memory.  More columns are bound by the vector unit's instructions, some 480 to 1100 for 128 tokens of a wave, which two waves a SIMD
+// issue one each 4.5 cycles: 24 ragged contexts with up to 3 rows of 7 x 4 heads, f16, capped and sloped, 131 us (2.2 TB/s), 62 for one
+// row of 4 x 4 heads in bf16.  (64 tokens at a time and three waves a SIMD: 117 us for 99, as each step has as much around it.)
 template <bool BF16, bool SHAPED, int REP, int CG>
 struct Wave {
   static constexpr int NP = Columns<BF16, SHAPED, kFewHead>::NP;
@@ -545,7 +562,8 @@ __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, SHAPED, REP,
                                       bool step, int solo, int count, int mine, int ticket, Slot slot) {
   constexpr int kShares = kAttnWaves / CG;
   const int share = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) / CG;
-  const bool alone = count == 1 && (step || kShares == 1);     // (pieces of one unit are joined in one way, whichever comes last: the sums' order is fixed)
+  // (pieces of one unit are joined in one way, whichever comes last: the sums' order is fixed)
+  const bool alone = count == 1 && (step || kShares == 1);
   if (alone && share != solo % kShares) return;
   w.begin(u);
   t0 = max(t0, w.seen.first);
@@ -600,7 +618,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
   __shared__ AttnLds lds;
   Wave<BF16, SHAPED, REP, CG> w(a);
   int solo = 0;
-  deal<kAttnThreads, kLeastTiles, kPieceTiles, kFewPad>(a, false, most_tiles(a), lead_of(a), [&](const Unit& u, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<kAttnThreads, kLeastTiles, kPieceTiles, kFewPad>(a, false, most_tiles(a), lead_of(a), [&](const Unit& u, int t0, int t1, int f, int count,
+                                                                                                  int mine, auto slot) {
     const int first = first_tile(a, u);
     piece(a, w, lds, u, t0 > 0 ? first + t0 : 0, first + t1, t1 - t0 <= kStep, solo, count, mine, f, slot);
     ++solo;
@@ -612,6 +631,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
 // Each wave has its own kRowGroups * 16 columns, and the workgroup's WAVES go through the tokens together, 64 at a time: waves fetch a
 // tile each, widen it and put it into LDS in operand order, while the 64 before it are taken; so a code is widened once for all
 // of them.  Values take their scales there.  Of eight waves four have the keys and four the values.
+// Bound by issue: about 330 vector instructions, 64 products and 33 trips to LDS a wave and stage, two waves a SIMD, vector unit and
+// matrix cores busy 55 % and 30 % of the time.  2 x 2048 rows of 32/8 heads behind 6144 tokens 510 us (940 TFLOP/s), in documents of
+// 5000 tokens 208 (700), 2 x 4096 rows from the start 340 (810).  (32 x 32 products: 229 for 210, as only two chains of them go at a time.)
 constexpr int kRowGroups = 2;
 constexpr int kStageTiles = 4;
 template <int WAVES>
@@ -632,7 +654,8 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
   const bool keys = wave < kStageTiles, values = WAVES == kStageTiles || !keys;
   Columns<BF16, SHAPED, kRowsHead> x[NQ];
   const bool grow = !windowed(a) && a.prefix_len == nullptr;
-  deal<WAVES * kWave, kLeastTiles, 0, kRowsPad>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count, int mine, auto slot) {
+  deal<WAVES * kWave, kLeastTiles, 0, kRowsPad>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count,
+                                                                                         int mine, auto slot) {
     Unit u = whole;                            // this wave's rows
     u.row0 += wave * rows;
     u.pos0 += wave * rows;
@@ -691,17 +714,9 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const u32 w = (u32)vc[half * 2 + (i >> 1)];
-          u32 two[2];
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            u32 lo, hi;
-            if ((i & 1) * 2 + y == 0) { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 0)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 0)); }
-            else if ((i & 1) * 2 + y == 1) { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 1)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 1)); }
-            else if ((i & 1) * 2 + y == 2) { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 2)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 2)); }
-            else { lo = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y], 3)); hi = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, e[2 * y + 1], 3)); }
-            two[y] = (lo & 0xffffu) | (hi & 0xffff0000u);
-          }
-          to_v[(half * kWave + i * 16) * 2] = (u64)two[1] << 32 | two[0];
+          const u32 first = (i & 1) ? pair<2>(w, e[0], e[1]) : pair<0>(w, e[0], e[1]);
+          const u32 second = (i & 1) ? pair<3>(w, e[2], e[3]) : pair<1>(w, e[2], e[3]);
+          to_v[(half * kWave + i * 16) * 2] = (u64)second << 32 | first;
         }
       }
     };
@@ -815,8 +830,9 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
   });
 }
 
-// How the columns that the rows of a sequence take, on the average, are laid out: copies of them in 16, or groups of 16 (0: waves with
-// rows of their own, of 4 or 8 waves)
+// How the columns that the rows of a sequence take, on the average, are laid out: copies of them in 16, or groups of 16 (0: workgroups
+// of 4 or 8 waves with rows of their own).  us: 30 x 3000 tokens, 4 columns: four copies 20.1, one 21.2.  16 x 6000 tokens of 8 heads, 64 columns:
+// four groups 73, 4 waves with rows 84; 96: 106, 91; 128: 113, 95, and 8 waves with rows 104; 160: 4 waves 144, 8 waves 127; 252: 149, 142.
 struct Shape { int copies, groups, waves; };
 static Shape shape_of(int T, int B, int G) {
   const int64_t want = (int64_t)((T + B - 1) / B) * G;
@@ -831,7 +847,8 @@ extern "C" int64_t kvd_q4_workspace_bytes(const kvd_q4_cache* c, const kvd_q8_ro
   if (int e = check_cache(c, r)) return e;
   static_assert(kAttnGroups * kAttnWaves * 4 <= kvd::q8::kTicketBytes, "a ticket for each wave of each workgroup");
   const Shape shape = shape_of(r->n_rows, r->n_seqs, c->n_q_heads / c->n_kv_heads);
-  return kvd::q8::kTicketBytes + (int64_t)kAttnGroups * 2 * 8 * kPartWords * (shape.groups ? shape.groups : kAttnWaves * kRowGroups);  // (8 waves: half as many workgroups)
+  // (with 8 waves half as many workgroups)
+  return kvd::q8::kTicketBytes + (int64_t)kAttnGroups * 2 * 8 * kPartWords * (shape.groups ? shape.groups : kAttnWaves * kRowGroups);
 }
 
 extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const void* q, int64_t q_stride, const kvd_q4_scores* f,

@@ -563,6 +563,10 @@ def _buffer(name: str, t: torch.Tensor, shape, dtype, device) -> torch.Tensor:
     return t
 
 
+# The handle of a GPU's current stream, without an object around it where torch has that (1.1 us of a call's 8)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _OnDevice:
     """Calls into the library with the tensors' GPU current, on `stream` or that GPU's current stream."""
 
@@ -572,7 +576,7 @@ class _OnDevice:
             raise ValueError(f"{name}: tensors on a GPU are wanted, got {device}")
         if stream is not None and stream.device != device:
             raise ValueError(f"{name}: the stream is on {stream.device}, the tensors on {device}")
-        handle = _stream_handle(stream or torch.cuda.current_stream(device.index))
+        handle = (_raw_stream(device.index) if stream is None else stream.cuda_stream) or None
         if torch.cuda.current_device() == device.index:
             st = getattr(self.lib, name)(*args, handle)
         else:
