@@ -585,7 +585,7 @@ int kvd_q8_attn(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* 
  *   pair i = elements (i, i + rot_dim/2), or (2i, 2i + 1) if interleaved:  (a, b) -> (a cos t - b sin t, a sin t + b cos t),
  *   t = pos[axis][row] * inv_freq[i], exact to 2^-24 of a turn for positions of any size (products of up to 2^29 turns)
  * The pairs are dealt to the axes in order: the first axis_pairs[0] turn by axis 0 and so on (time, height and width of an image's
- * patches; one axis for text).  The sum of squares has to be finite in fp32.
+ * patches; one axis for text).  The sum of squares has to be finite in fp32 (and not below its normal numbers where eps is 0).
  */
 typedef struct {
   int32_t n_q_heads, n_kv_heads;   /* 1..65536 each */
@@ -636,7 +636,7 @@ typedef struct {
 
 /* What becomes of a row's scores.  A struct of zeros (or NULL in its place) changes nothing. */
 typedef struct {
-  float softcap;               /* > 0: logits x become softcap * tanh(x / softcap) */
+  float softcap;               /* > 0: logits x become softcap * tanh(x / softcap); up to 2^96 */
   int32_t window;              /* > 0: a row at position p sees tokens from p - window + 1 on */
   const float* slopes;         /* dev [Hq] or NULL: slope * |p - t| is taken off the logit of token t (after the cap) */
   const int32_t* row_from;     /* dev [T] or NULL: first position that a row sees (its document's first token) */
@@ -664,9 +664,10 @@ int64_t kvd_q4_workspace_bytes(const kvd_q4_cache* cache, const kvd_q8_rows* row
  *   q [T][Hq][D] kv_dtype, rows q_stride elements apart;  out [T][Hq][D] kv_dtype;  lse [T][Hq] fp32 or NULL.
  * out = softmax(f(scale * q K^T)) V, lse = log sum exp of the logits; 0 and -infinity where a row sees nothing.  Sums, maxima and
  * accumulators are fp32; the weights that multiply V have 16 bits where kv_dtype is f16 (off by 2^-16 of themselves at most), 8 (2^-8)
- * where it is bf16.  Relative to the row's largest weight, a weight times its value's scale is lost below 2^-90.  The
- * products q K^T of what a row sees, and its logits, have to be finite in fp32; a row and head with a query that is not finite gives
- * NaN.  Rows without a sequence are left as they were.  kv_len and row_start must be those of row_seq and row_pos. */
+ * where it is bf16.  A capped logit is off by 2^-20 of the cap at most, or of itself where the cap is above 64.  Relative to the row's
+ * largest weight, a weight times its value's scale is lost below 2^-90.  The products q K^T of what a row sees, and its logits, have to
+ * be finite in fp32; a row and head with a query that is not finite gives NaN.  Rows without a sequence are left as they were.  kv_len
+ * and row_start must be those of row_seq and row_pos. */
 int kvd_q4_attn(const kvd_q4_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, const kvd_q4_scores* scores,
                 void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 

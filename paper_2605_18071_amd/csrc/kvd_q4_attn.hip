@@ -36,6 +36,9 @@ constexpr int kFewPad = 16, kRowsPad = 24;
 // Tiles of a workgroup where there are few, so that most units need no joining: 30 x 3000 tokens of 8 heads 20 us; with 32 26, with 128
 // 25.  4 x 2500: 13.3, 12.8, 16.0
 constexpr int kPieceTiles = 64;
+// What becomes of logits, in kernels of their own (a branch for large caps in the ones without: f16 drafts 136 us for 123)
+constexpr int kPlain = 0, kShaped = 1, kShapedFar = 2;         // nothing; a cap, slopes; a cap above kNearCap, slopes
+constexpr float kNearCap = 64;                 // up to here a cap's logits are off by 2^-20 of the cap, beyond it by 2^-20 of themselves
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 constexpr int kPartWords = 16 * kWave + 16;    // 8-byte words of 16 columns' partial result: accumulators, then a maximum and a sum a column
 constexpr float kLowest = -3.0e38f, kSlack = 8.f;
@@ -84,6 +87,13 @@ __device__ __forceinline__ float sum_of_column(float x) {
 __device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ u32 byte_of(u32 w, int i) { return w >> (8 * i) & 255; }
 
+// tanh(x ln 2 / 2) / 2, off by 2^-21 of itself, where a cap is so large that 2^-24 of it would show.  Near 0 by its continued fraction
+// y / (1 + y^2 / (3 + y^2 / (5 + y^2 / (7 + y^2 / 9)))), off by y^10 / 9823275 of itself: below 2^-27 where it is taken
+__device__ __forceinline__ float half_tanh(float x) {
+  const float y = x * (kLn2 / 2), z = y * y;
+  const float near = y * 0.5f * (945.f + z * (105.f + z)) * __builtin_amdgcn_rcpf(945.f + z * (420.f + z * 15.f));
+  return fabsf(y) < 0.75f ? near : 0.5f + __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(x));
+}
 // Eight codes to an operand, times the scale
 __device__ __forceinline__ bf16x8 widen(int codes, float scale) {
   const u32 w = (u32)codes;
@@ -140,7 +150,7 @@ struct Seen {
 };
 
 // Sixteen columns: lane (c, n) = (lane / 16, lane % 16) has elements 16 i + 4 c + 0..3 of column n in o[i]
-template <bool BF16, bool SHAPED, int HEAD>
+template <bool BF16, int SHAPE, int HEAD>
 struct Columns {
   static constexpr float kHead = HEAD;
   static constexpr int NP = BF16 ? 1 : 2;      // parts of bf16 that a number of q's type has
@@ -192,19 +202,26 @@ struct Columns {
       for (int i = 0; i < 4; ++i) q[i][0] = __builtin_bit_cast(bf16x8, make_uint4(~0u, ~0u, ~0u, ~0u));
     clear();
   }
-  // Products of N x 4 tokens to logits in powers of two, but for the factor that is returned, and less cap_out; at(j): the position of
+  // Products of N x 4 tokens to logits in powers of two, but for the factor that is returned, and less cap_out where that is SHAPE kShaped's; at(j): the position of
   // the first four of s[j]
   template <int N, class At>
   __device__ __forceinline__ float logits(const AttnArgs& a, f32x4 (&s)[N], At at) const {
     float scale = a.scale_log2;
-    if constexpr (!SHAPED) return scale;
+    if constexpr (SHAPE == kPlain) return scale;
     if (a.cap_in != 0.f) {
       scale = 2.f * a.cap_out;
+      if constexpr (SHAPE == kShaped) {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)            // tanh x = 1 - 2 / (e^2x + 1)
-          s[j][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[j][i] * a.cap_in));
+          for (int i = 0; i < 4; ++i)          // tanh x = 1 - 2 / (e^2x + 1)
+            s[j][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[j][i] * a.cap_in));
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[j][i] = half_tanh(s[j][i] * a.cap_in);
+      }
     }
     if (a.slopes) {
       const float far = (float)(at(0) - pos);  // (below 2^24: exact, and its sums)
@@ -298,7 +315,7 @@ __device__ __forceinline__ Seen seen_of(int (&see)[4]) {
 }
 
 // N elements of a column's result over all tokens; the weights were taken times 2^-DOWN
-template <bool BF16, int DOWN, int N>
+template <bool BF16, int SHAPE, int DOWN, int N>
 __device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, int head, int d, const float (&v)[N], float m, float l) {
   const size_t at = (size_t)(u.row0 + r) * a.H * a.G + u.h * a.G + head;
   const float inv = l == 0.f ? 0.f : two_to(DOWN) / l;
@@ -307,7 +324,7 @@ __device__ __forceinline__ void emit(const AttnArgs& a, const Unit& u, int r, in
   for (int i = 0; i < N / 2; ++i) w[i] = pack2<BF16>(l == 0.f ? 0.f : v[2 * i] * inv, l == 0.f ? 0.f : v[2 * i + 1] * inv);
   if constexpr (N == 8) *reinterpret_cast<uint4*>(a.out + at * kHeadDim + d) = make_uint4(w[0], w[1], w[2], w[3]);
   else *reinterpret_cast<uint2*>(a.out + at * kHeadDim + d) = make_uint2(w[0], w[1]);
-  if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l) + a.cap_out) * kLn2;
+  if (a.lse != nullptr && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l) + (SHAPE == kShapedFar ? 0.f : a.cap_out)) * kLn2;
 }
 
 // Tiles of a sequence's pages
@@ -337,13 +354,13 @@ __device__ __forceinline__ const unsigned char* tile_at(const AttnArgs& a, u32 l
 // to memory.  More columns are bound by the vector unit's instructions, some 480 to 1100 for 128 tokens of a wave, which two waves a SIMD
 // issue one each 4.5 cycles: 24 ragged contexts with up to 3 rows of 7 x 4 heads, f16, capped and sloped, 131 us (2.2 TB/s), 62 for one
 // row of 4 x 4 heads in bf16.  (64 tokens at a time and three waves a SIMD: 117 us for 99, as each step has as much around it.)
-template <bool BF16, bool SHAPED, int REP, int CG>
+template <bool BF16, int SHAPE, int REP, int CG>
 struct Wave {
-  static constexpr int NP = Columns<BF16, SHAPED, kFewHead>::NP;
+  static constexpr int NP = Columns<BF16, SHAPE, kFewHead>::NP;
   static constexpr int kCols = 16 / REP;       // columns that differ
   static constexpr int kGroups = 4 / REP;      // of V's groups of 32 columns, those that a lane weighs
   static_assert(CG == 1 || REP == 1, "");
-  Columns<BF16, SHAPED, kFewHead> x;
+  Columns<BF16, SHAPE, kFewHead> x;
   Seen seen;
 
   const AttnArgs& a;
@@ -504,9 +521,9 @@ struct AttnLds {
 };
 
 // The results of the waves that share columns as one: with to_slot < 0 to the output, else there
-template <bool BF16, bool SHAPED, int REP, int CG>
-__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, SHAPED, REP, CG>& w, AttnLds& lds, int to_slot) {
-  typedef Wave<BF16, SHAPED, REP, CG> W;
+template <bool BF16, int SHAPE, int REP, int CG>
+__device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, SHAPE, REP, CG>& w, AttnLds& lds, int to_slot) {
+  typedef Wave<BF16, SHAPE, REP, CG> W;
   const int tid = threadIdx.x, wave = tid / kWave;
   __syncthreads();                             // (what was there has been read)
   if (w.c == 0) {
@@ -541,7 +558,7 @@ __device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, 
 #pragma unroll
         for (int i = g; i < kAttnWaves; i += CG) v[y] += lds.o[i][n][d + y];
       }
-      if (to_slot < 0) emit<BF16, kFewDown>(a, w.u, r, head, d, v, top, L);
+      if (to_slot < 0) emit<BF16, SHAPE, kFewDown>(a, w.u, r, head, d, v, top, L);
       else {
         u64* part = w.part_of(to_slot, g);
         const int i = d / 16;
@@ -557,8 +574,8 @@ __device__ __forceinline__ void merge_waves(const AttnArgs& a, const Wave<BF16, 
 // Tiles [t0, t1) of a unit: by all waves, or, if they are one step (`step`), by those of turn `solo` alone.  Its result goes to the output if it is
 // all of the unit (count == 1), else to slot `mine` of the partial results, which the last of the `count` pieces to arrive
 // joins, in their order; slot(i) is the i-th one's number.
-template <bool BF16, bool SHAPED, int REP, int CG, class Slot>
-__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, SHAPED, REP, CG>& w, AttnLds& lds, const Unit& u, int t0, int t1,
+template <bool BF16, int SHAPE, int REP, int CG, class Slot>
+__device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, SHAPE, REP, CG>& w, AttnLds& lds, const Unit& u, int t0, int t1,
                                       bool step, int solo, int count, int mine, int ticket, Slot slot) {
   constexpr int kShares = kAttnWaves / CG;
   const int share = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) / CG;
@@ -581,7 +598,7 @@ __device__ __forceinline__ void piece(const AttnArgs& a, Wave<BF16, SHAPED, REP,
     for (int i = 0; i < 8; ++i) {
       if (!w.has(i)) continue;
       const float v[4] = {w.x.o[i][0], w.x.o[i][1], w.x.o[i][2], w.x.o[i][3]};
-      emit<BF16, kFewDown>(a, u, r, head, i * 16 + w.c * 4, v, w.x.m, w.x.l);
+      emit<BF16, SHAPE, kFewDown>(a, u, r, head, i * 16 + w.c * 4, v, w.x.m, w.x.l);
     }
     return;
   }
@@ -613,10 +630,10 @@ __device__ __forceinline__ auto lead_of(const AttnArgs& a) {
   return [&a](int row0) { return a.row_from && row0 < a.T ? max(a.row_from[row0], 0) / kTile : 0; };
 }
 
-template <bool BF16, bool SHAPED, int REP, int CG>
+template <bool BF16, int SHAPE, int REP, int CG>
 __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
   __shared__ AttnLds lds;
-  Wave<BF16, SHAPED, REP, CG> w(a);
+  Wave<BF16, SHAPE, REP, CG> w(a);
   int solo = 0;
   deal<kAttnThreads, kLeastTiles, kPieceTiles, kFewPad>(a, false, most_tiles(a), lead_of(a), [&](const Unit& u, int t0, int t1, int f, int count,
                                                                                                   int mine, auto slot) {
@@ -644,15 +661,15 @@ struct RowsLds {
   int first[WAVES], behind[WAVES];
 };
 
-template <bool BF16, bool SHAPED, int WAVES>
+template <bool BF16, int SHAPE, int WAVES>
 __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs a) {
-  constexpr int NQ = kRowGroups, NP = Columns<BF16, SHAPED, kRowsHead>::NP;
+  constexpr int NQ = kRowGroups, NP = Columns<BF16, SHAPE, kRowsHead>::NP;
   __shared__ RowsLds<WAVES> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, c = lane >> 4, n = lane & 15;
   const int rows = a.R / WAVES;                // of a wave
   const int tile = wave % kStageTiles;         // of a stage, the one that this wave fetches
   const bool keys = wave < kStageTiles, values = WAVES == kStageTiles || !keys;
-  Columns<BF16, SHAPED, kRowsHead> x[NQ];
+  Columns<BF16, SHAPE, kRowsHead> x[NQ];
   const bool grow = !windowed(a) && a.prefix_len == nullptr;
   deal<WAVES * kWave, kLeastTiles, 0, kRowsPad>(a, grow, most_tiles(a), lead_of(a), [&](const Unit& whole, int t0, int t1, int f, int count,
                                                                                          int mine, auto slot) {
@@ -824,7 +841,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float v[4] = {x[g].o[i][0], x[g].o[i][1], x[g].o[i][2], x[g].o[i][3]};
-          emit<BF16, 0>(a, u, r, col - r * a.G, i * 16 + c * 4, v, x[g].m, x[g].l);
+          emit<BF16, SHAPE, 0>(a, u, r, col - r * a.G, i * 16 + c * 4, v, x[g].m, x[g].l);
         }
       }
   });
@@ -864,14 +881,14 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
   AttnArgs a = {};
   a.scale_log2 = fminf(fmaxf((c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e, 0x1p-126f), 0x1.fffffep127f);
   if (f) {
-    if (!(f->softcap >= 0.f) || isinf(f->softcap)) return KVD_ERR_ARG;
+    if (!(f->softcap >= 0.f) || f->softcap > 0x1p96f) return KVD_ERR_ARG;
     if (f->window < 0) return KVD_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(f->slopes) | reinterpret_cast<uintptr_t>(f->row_from) | reinterpret_cast<uintptr_t>(f->prefix_len)) & 3)
       return KVD_ERR_ARG;
     if (f->softcap > 0.f) {
       a.cap_in = 2.f * a.scale_log2 / f->softcap;
       a.cap_out = f->softcap * kLog2e;
-      if (!(a.cap_in > 0.f) || isinf(a.cap_in) || isinf(a.cap_out)) return KVD_ERR_ARG;
+      if (!(a.cap_in >= 0x1p-126f) || isinf(a.cap_in)) return KVD_ERR_ARG;
     }
     a.window = f->window; a.slopes = f->slopes; a.row_from = f->row_from; a.prefix_len = f->prefix_len;
   }
@@ -891,8 +908,9 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
   a.W = shape.groups || shape.waves == kAttnWaves ? kAttnGroups : kAttnGroups / 2;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel, int waves = kAttnWaves) { hipLaunchKernelGGL(kernel, dim3(a.W), dim3(waves * kvd::kWave), 0, s, a); };
-  auto typed = [&](auto bf16, auto shaped) {
-    constexpr bool B = decltype(bf16)::value, S = decltype(shaped)::value;
+  auto typed = [&](auto bf16, auto shape_of_scores) {
+    constexpr bool B = decltype(bf16)::value;
+    constexpr int S = decltype(shape_of_scores)::value;
     if (shape.copies == 4) go(q4_attn_kernel<B, S, 4, 1>);
     else if (shape.copies == 2) go(q4_attn_kernel<B, S, 2, 1>);
     else if (shape.groups == 1) go(q4_attn_kernel<B, S, 1, 1>);
@@ -901,11 +919,11 @@ extern "C" int kvd_q4_attn(const kvd_q4_cache* c, const kvd_q8_rows* r, const vo
     else if (shape.waves == 4) go(q4_attn_rows_kernel<B, S, 4>);
     else go(q4_attn_rows_kernel<B, S, 8>, 8);
   };
-  const bool shaped = a.cap_in != 0.f || a.slopes != nullptr;
-  if (c->kv_dtype == KVD_BF16) {
-    if (shaped) typed(std::true_type{}, std::true_type{}); else typed(std::true_type{}, std::false_type{});
-  } else {
-    if (shaped) typed(std::false_type{}, std::true_type{}); else typed(std::false_type{}, std::false_type{});
-  }
+  auto shaped = [&](auto bf16) {
+    if (a.cap_in == 0.f && a.slopes == nullptr) typed(bf16, std::integral_constant<int, kPlain>{});
+    else if (a.cap_in == 0.f || f->softcap <= kNearCap) typed(bf16, std::integral_constant<int, kShaped>{});
+    else typed(bf16, std::integral_constant<int, kShapedFar>{});
+  };
+  if (c->kv_dtype == KVD_BF16) shaped(std::true_type{}); else shaped(std::false_type{});
   return launched();
 }

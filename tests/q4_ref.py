@@ -114,6 +114,7 @@ class Row:
         z = x @ k.T * scale
         if cap:
             z = cap * np.tanh(z / cap)
+        self.capped = np.abs(z).max(-1)
         if slopes is not None:
             z = z - slopes[:, None] * np.abs(pos - t)[None, :]
         top = z.max(-1, keepdims=True)

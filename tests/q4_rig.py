@@ -73,8 +73,8 @@ class Step:
          + what fp32 cannot hold: weights times scales are kept with the row's largest weight at 2^-36, and what is below fp32's least
            normal 2^-126 may be lost: 2^(36 - 126) of a code of up to 6 for each token                            n 2^-87
          + f16: below its normal numbers                                                               2^-25.
-        Logits: products of 128 elements and their sums in fp32 (2^-17 sum |q k| scale), a cap's exponent and reciprocal (2^-20 cap), a bias's
-        rounding (2^-22), the exponent's argument (2^-23 of it) and 2^-20."""
+        Logits: products of 128 elements and their sums in fp32 (2^-17 sum |q k| scale), a cap's exponent and reciprocal (2^-20 of the
+        cap; above 64 of the logit), a bias's rounding (2^-22), the exponent's argument (2^-23 of it) and 2^-20."""
         ref, table = self.ref(), self.table if table is None else table
         h = torch.finfo(torch_type(self.dtype)).eps / 2
         r = 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -16
@@ -95,7 +95,7 @@ class Step:
                 if x.empty:
                     assert (got == 0).all() and (ld is None or (ld[row, heads] == -np.inf).all()), (row, hd)
                     continue
-                dx = 2.0 ** -17 * x.products + 2.0 ** -20 * (1 + softcap) + 2.0 ** -22 * x.bias + 2.0 ** -23 * x.largest
+                dx = 2.0 ** -17 * x.products + 2.0 ** -20 * (1 + (softcap if softcap <= 64 else x.capped)) + 2.0 ** -22 * x.bias + 2.0 ** -23 * x.largest
                 tol = h * np.abs(x.out) + (r + 2 * dx[:, None] + 2.0 ** -17) * x.mass + x.n * 2.0 ** -87
                 if self.dtype == "f16":
                     tol = tol + 2.0 ** -25

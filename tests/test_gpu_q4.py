@@ -234,6 +234,16 @@ def test_attend_with_scores_of_all_kinds(dtype, kw, lens, news, Gq):
     s.check(q, out, lse, rows=range(0, s.real, 1 + s.real // 40), **made)
 
 
+@pytest.mark.parametrize("softcap", [64.0, 65.0, 300.0, 3e4, 1e6, 2.0 ** 96])
+@pytest.mark.parametrize("lens,news", [([700, 130], [1, 1]), ([300, 90], [9, 3]), ([200, 31], [90, 40])])
+def test_large_caps(softcap, lens, news):
+    """Logits of a few and of some hundreds, each as exact as without the cap however large that is."""
+    for size in (1.0, 30.0):
+        s = Step(lens, news, H=2, G=4, dtype="f16", seed=3)
+        q = s.query(size)
+        s.check(q, *s.attend(q, softcap=softcap), softcap=softcap, rows=range(0, s.real, 1 + s.real // 20))
+
+
 @pytest.mark.parametrize("news", [[1, 1], [3, 2], [40, 7]])
 def test_rows_that_see_nothing(news):
     s = Step([200, 60], news, H=2, G=3, seed=6)

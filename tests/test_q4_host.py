@@ -73,7 +73,7 @@ def test_pointers_strides_and_workspaces():
         return attn(scores=C.byref(kvd.KvdQ4Scores(cap, window, slopes, row_from, prefix_len)), n=0)
 
     assert scores() == scores(cap=30.0, window=9, slopes=P, row_from=P, prefix_len=P) == kvd.ERR_CAPACITY    # nothing but the workspace is wrong
-    assert scores(cap=-1.0) == scores(cap=float("nan")) == scores(cap=float("inf")) == scores(cap=1e-45) == kvd.ERR_ARG
+    assert scores(cap=-1.0) == scores(cap=float("nan")) == scores(cap=float("inf")) == scores(cap=1e-45) == scores(cap=1e29) == kvd.ERR_ARG
     assert scores(window=-1) == kvd.ERR_SHAPE
     assert scores(slopes=P + 1) == scores(row_from=P + 2) == scores(prefix_len=P + 3) == kvd.ERR_ARG
 
