@@ -352,14 +352,19 @@ __device__ __forceinline__ const unsigned char* tile_at(const AttnArgs& a, u32 l
 // and have 16 columns each.
 // One row a sequence is bound by the memory: 16 x 32768 tokens of 8 heads 99 us (5.8 TB/s); 4 x 1000 tokens 10.9 us by its chain of trips
 // to memory.  More columns are bound by the vector unit's instructions, some 480 to 1100 for 128 tokens of a wave, which two waves a SIMD
-// issue one each 4.5 cycles: 24 ragged contexts with up to 3 rows of 7 x 4 heads, f16, capped and sloped, 131 us (2.2 TB/s), 62 for one
-// row of 4 x 4 heads in bf16.  (64 tokens at a time and three waves a SIMD: 117 us for 99, as each step has as much around it.)
+// issue one each 4.5 cycles: 24 ragged contexts with up to 3 rows of 7 x 4 heads, f16, capped and sloped, 121 us (2.4 TB/s), 64 for one
+// row in bf16.  (64 tokens at a time and three waves a SIMD: 117 us for 99, as each step has as much around it.)
+// What a lane would not need all the time lies in LDS, its wave's scales of values and, where registers are short, its queries: spilled
+// ones came back behind the loads on their way, and the wait for them was one for all of those (the drafts 133 us, with the queries
+// alone in LDS 126).
 template <bool BF16, int SHAPE, int REP, int CG>
 struct Wave {
   static constexpr int NP = Columns<BF16, SHAPE, kFewHead>::NP;
   static constexpr int kCols = 16 / REP;       // columns that differ
   static constexpr int kGroups = 4 / REP;      // of V's groups of 32 columns, those that a lane weighs
   static_assert(CG == 1 || REP == 1, "");
+  // (bf16 with a cap, 16 x 32768 tokens 104 us, 112 with them in registers)
+  static constexpr bool kPutBy = !BF16 || SHAPE != kPlain;
   Columns<BF16, SHAPE, kFewHead> x;
   Seen seen;
 
@@ -371,6 +376,11 @@ struct Wave {
       : a(a_), lane(threadIdx.x % kWave), c((threadIdx.x % kWave) >> 4), n(threadIdx.x & 15),
         cg(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) % CG) {}
 
+  // Queries, where a step takes them from LDS
+  static __device__ __forceinline__ uint4* put_by() {
+    __shared__ uint4 at[kPutBy ? 4 * NP * kAttnThreads : 1];
+    return at + threadIdx.x;
+  }
   // Row of the unit and head of the group of column col
   __device__ __forceinline__ bool column(int col, int& r, int& head) const {
     r = col / a.G;
@@ -390,13 +400,16 @@ struct Wave {
     const bool ok = column(cg * 16 + n % kCols, r, head);
     x.begin(a, u, ok, r, head, len, prefix, see);
     seen = seen_of(see);
+    if constexpr (kPutBy)
+#pragma unroll
+      for (int i = 0; i < 4 * NP; ++i) put_by()[i * kAttnThreads] = __builtin_bit_cast(uint4, x.q[i / NP][i % NP]);
   }
 
   // ---- what is on its way
 
   i32x4 k[8], v[8];
   u32 ks[2];
-  i32x4 vs[kGroups][2];
+  u64 vs;                                      // of the 32 tokens that the lanes (c, *) have, scales of 8 values, of group n % 8 / 2
   u32 line, line_next;                         // of the step's tile lane % 8
   int block_next;                              // of the step after that
 
@@ -417,18 +430,23 @@ struct Wave {
       v[2 * i] = load_codes<CG == 1>(at0 + kValues + n * 16 + i * 256);
       v[2 * i + 1] = load_codes<CG == 1>(at1 + kValues + n * 16 + i * 256);
     }
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      const int group = i * REP + (REP > 1 ? n / kCols : 0);
-      vs[i][0] = load_scales(at0 + kValueScales + group * 16);
-      vs[i][1] = load_scales(at1 + kValueScales + group * 16);
-    }
+    vs = *reinterpret_cast<const u64*>((n < 8 ? at0 : at1) + kValueScales + (n & 7) * 8);
+  }
+  // In LDS, for each c: scales of two tiles, four groups and 16 tokens
+  static __device__ __forceinline__ u64* scales_of(int wave) {
+    __shared__ __align__(16) u64 at[kAttnThreads];
+    return at + wave * kWave;
   }
 
   // ---- the step of tiles [t0, t0 + 8)
 
   // Row r of the products of tile j is token 32 (r / 4) + 4 j + r % 4 of the step, so that lane (c, n) gets tokens 32 c + 0..31 of column n
   __device__ __forceinline__ void scores(f32x4 (&s)[8]) {
+    bf16x8 q[4][NP];
+    int none = 0;
+    asm volatile("" : "+v"(none));             // (taken anew each time)
+#pragma unroll
+    for (int i = 0; i < 4 * NP; ++i) q[i / NP][i % NP] = kPutBy ? __builtin_bit_cast(bf16x8, put_by()[i * kAttnThreads + none]) : x.q[i / NP][i % NP];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float scale = two_to((int)byte_of(ks[j / 4], j % 4) - kBias);
@@ -437,7 +455,7 @@ struct Wave {
       for (int i = 0; i < 4; ++i) {
         const bf16x8 A = widen(k[j][i], scale);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) s[j] = mfma32(A, x.q[i][p], s[j]);
+        for (int p = 0; p < NP; ++p) s[j] = mfma32(A, q[i][p], s[j]);
       }
     }
   }
@@ -446,13 +464,15 @@ struct Wave {
   template <int X>
   __device__ __forceinline__ void weigh(const u16x2 (&p)[4][NP][4]) {
     const u32 times = 0x10001u * (u32)(0x10000 - 128), most = 0x10001u * ((kBias + kFewDown) << 7);
+    const u64* from = scales_of(threadIdx.x / kWave) + c * 16 + (X * REP + (REP > 1 ? n / kCols : 0)) * 2;
+    const i32x4 scales[2] = {*reinterpret_cast<const i32x4*>(from), *reinterpret_cast<const i32x4*>(from + 8)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {              // eight of the lane's tokens
       bf16x8 B[NP];
       u16x2 w[NP][4];
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        const u32 bytes = __builtin_amdgcn_perm(0, (u32)vs[X][i >> 1][(i & 1) * 2 + (y >> 1)], y & 1 ? 0x0c030c02 : 0x0c010c00);
+        const u32 bytes = __builtin_amdgcn_perm(0, (u32)scales[i >> 1][(i & 1) * 2 + (y >> 1)], y & 1 ? 0x0c030c02 : 0x0c010c00);
         const u16x2 down = mad_pair(bytes, times, most);
 #pragma unroll
         for (int z = 0; z < NP; ++z) w[z][y] = __builtin_elementwise_sub_sat(p[i][z][y], down);
@@ -500,6 +520,7 @@ struct Wave {
         u16x2 w[4][NP][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) weights<NP>(p + 8 * i, w[i]);
+        scales_of(threadIdx.x / kWave)[lane] = vs;
         each_of<kGroups>([&](auto g) { weigh<decltype(g)::value>(w); });
         __builtin_amdgcn_sched_barrier(0);
         line = line_next;
@@ -848,8 +869,8 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
 }
 
 // How the columns that the rows of a sequence take, on the average, are laid out: copies of them in 16, or groups of 16 (0: workgroups
-// of 4 or 8 waves with rows of their own).  us: 30 x 3000 tokens, 4 columns: four copies 20.1, one 21.2.  16 x 6000 tokens of 8 heads, 64 columns:
-// four groups 73, 4 waves with rows 84; 96: 106, 91; 128: 113, 95, and 8 waves with rows 104; 160: 4 waves 144, 8 waves 127; 252: 149, 142.
+// of 4 or 8 waves with rows of their own).  us: 30 x up to 3000 tokens, 4 columns: four copies 20.5, one 21.1.  16 x 6000 tokens of 8 heads, 64 columns:
+// four groups 69, 4 waves with rows 84; 96: 106, 91; 128: 113, 95, and 8 waves with rows 104; 160: 4 waves 144, 8 waves 127; 252: 149, 142.
 struct Shape { int copies, groups, waves; };
 static Shape shape_of(int T, int B, int G) {
   const int64_t want = (int64_t)((T + B - 1) / B) * G;
