@@ -202,8 +202,8 @@ struct Columns {
       for (int i = 0; i < 4; ++i) q[i][0] = __builtin_bit_cast(bf16x8, make_uint4(~0u, ~0u, ~0u, ~0u));
     clear();
   }
-  // Products of N x 4 tokens to logits in powers of two, but for the factor that is returned, and less cap_out where that is SHAPE kShaped's; at(j): the position of
-  // the first four of s[j]
+  // Products of N x 4 tokens to logits in powers of two, but for the factor that is returned, and less cap_out (not in kShapedFar);
+  // at(j): the position of the first four of s[j]
   template <int N, class At>
   __device__ __forceinline__ float logits(const AttnArgs& a, f32x4 (&s)[N], At at) const {
     float scale = a.scale_log2;
@@ -390,7 +390,9 @@ struct Wave {
   // whether this lane's accumulators of 16 columns of V are of the weights that were made for them
   __device__ __forceinline__ bool has(int i) const { return REP == 1 || (i >> 1) % REP == n / kCols; }
   // Lane that has column col's accumulators of 16 columns of V
-  __device__ __forceinline__ int lane_of(int i, int col, int quarter) const { return quarter * 16 + (REP == 1 ? col : col % kCols + (i >> 1) % REP * kCols); }
+  __device__ __forceinline__ int lane_of(int i, int col, int quarter) const {
+    return quarter * 16 + (REP == 1 ? col : col % kCols + (i >> 1) % REP * kCols);
+  }
 
   __device__ __forceinline__ void begin(const Unit& unit) {
     u = unit;
@@ -645,7 +647,9 @@ __device__ __forceinline__ int most_tiles(const AttnArgs& a) {
   return windowed(a) ? (int)min(((long long)a.window + a.R + 2 * kTile - 3) / kTile, (long long)q8::kAllTiles) : q8::kAllTiles;
 }
 // Where its tiles are counted from: a unit's first piece has what lies before that too
-__device__ __forceinline__ int first_tile(const AttnArgs& a, const Unit& u) { return max(u.lead, windowed(a) ? max(u.pos0 - a.window + 1, 0) / kTile : 0); }
+__device__ __forceinline__ int first_tile(const AttnArgs& a, const Unit& u) {
+  return max(u.lead, windowed(a) ? max(u.pos0 - a.window + 1, 0) / kTile : 0);
+}
 // Tiles of a sequence that its first row does not see, and no other row as a rule
 __device__ __forceinline__ auto lead_of(const AttnArgs& a) {
   return [&a](int row0) { return a.row_from && row0 < a.T ? max(a.row_from[row0], 0) / kTile : 0; };
@@ -869,8 +873,9 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
 }
 
 // How the columns that the rows of a sequence take, on the average, are laid out: copies of them in 16, or groups of 16 (0: workgroups
-// of 4 or 8 waves with rows of their own).  us: 30 x up to 3000 tokens, 4 columns: four copies 20.5, one 21.1.  16 x 6000 tokens of 8 heads, 64 columns:
-// four groups 69, 4 waves with rows 84; 96: 106, 91; 128: 113, 95, and 8 waves with rows 104; 160: 4 waves 144, 8 waves 127; 252: 149, 142.
+// of 4 or 8 waves with rows of their own).  us: 30 x up to 3000 tokens, 4 columns: four copies 20.5, one 21.1.  16 x 6000 tokens of 8
+// heads, 64 columns: four groups 69, 4 waves with rows 84; 96: 106, 91; 128: 113, 95, and 8 waves with rows 104; 160: 4 waves 144, 8
+// waves 127; 252: 149, 142.
 struct Shape { int copies, groups, waves; };
 static Shape shape_of(int T, int B, int G) {
   const int64_t want = (int64_t)((T + B - 1) / B) * G;
