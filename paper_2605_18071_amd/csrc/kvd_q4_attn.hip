@@ -11,9 +11,9 @@
 // One pass with a running reference m and sum l of a column: p = 2^(x - m).  m is HEAD above the largest logit when it is set, and
 // is raised only when a logit passes that by more than kSlack, so that the accumulators are rarely touched.  What multiplies values
 // of up to 2^128 stays below 2^-28, so that 2^24 of them have finite sums.
-// bf16: weights are rounded to bf16, by 2^-8 of themselves at most, like their output (16 bits would cost 4 % at 16 x 32768 tokens and 8 %
-// where contexts are short).  f16, whose outputs would show it: a second product takes what the rounding left (2^-16), and the
-// first one has the queries in two parts of bf16 too.
+// Weights have 16 bits: a second product takes what rounding them to bf16 left, which is off by 2^-16 of a weight at most.  (Without it
+// outputs in bf16 are off by 2.1e-3 to 2.3e-3 of their norm instead of the 1.6e-3 of their own rounding, and it is 100 us for 104 at 16 x
+// 32768 tokens, 11.3 for 12.2 where contexts are short, 513 for 665 where rows are many.)  f16 has the queries in two parts of bf16 too.
 #include "kvd_q4.h"
 #include "kvd_q8_deal.h"
 
@@ -41,6 +41,7 @@ constexpr int kPlain = 0, kShaped = 1, kShapedFar = 2;         // nothing; a cap
 constexpr float kNearCap = 64;                 // up to here a cap's logits are off by 2^-20 of the cap, beyond it by 2^-20 of themselves
 constexpr int kColFloats = kHeadDim + 4;       // a column in LDS
 constexpr int kPartWords = 16 * kWave + 16;    // 8-byte words of 16 columns' partial result: accumulators, then a maximum and a sum a column
+constexpr int kWeightParts = 2;                // operands of bf16 that a weight has: rounded, or cut, and what that left
 constexpr float kLowest = -3.0e38f, kSlack = 8.f;
 constexpr int kFewHead = -90, kRowsHead = 36, kFewDown = 126;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -129,17 +130,14 @@ __device__ __forceinline__ u16x2 mad_pair(u32 a, u32 b, u32 c) {
   asm("v_pk_mad_u16 %0, %1, %2, %3" : "=v"(x) : "v"(a), "s"(b), "v"(c));
   return __builtin_bit_cast(u16x2, x);
 }
-// Eight weights, none of them negative, to NP operands whose parts are not negative either: rounded to bf16, or cut, and what that left
-template <int NP>
-__device__ __forceinline__ void weights(const float* p, u16x2 (&to)[NP][4]) {
+// Eight weights, none of them negative, to operands whose parts are not negative either: cut to bf16, and what that left, rounded: off by
+// 2^-16 of themselves at most
+__device__ __forceinline__ void weights(const float* p, u16x2 (&to)[kWeightParts][4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float a = p[2 * i], b = p[2 * i + 1];
-    if constexpr (NP == 1) to[0][i] = __builtin_bit_cast(u16x2, pack2<true>(a, b));
-    else {
-      to[0][i] = __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(as_u32(b), as_u32(a), 0x07060302));
-      to[1][i] = __builtin_bit_cast(u16x2, pack2<true>(a - as_f32(as_u32(a) & 0xffff0000u), b - as_f32(as_u32(b) & 0xffff0000u)));
-    }
+    to[0][i] = __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(as_u32(b), as_u32(a), 0x07060302));
+    to[1][i] = __builtin_bit_cast(u16x2, pack2<true>(a - as_f32(as_u32(a) & 0xffff0000u), b - as_f32(as_u32(b) & 0xffff0000u)));
   }
 }
 
@@ -363,8 +361,8 @@ struct Wave {
   static constexpr int kCols = 16 / REP;       // columns that differ
   static constexpr int kGroups = 4 / REP;      // of V's groups of 32 columns, those that a lane weighs
   static_assert(CG == 1 || REP == 1, "");
-  // (bf16 with a cap, 16 x 32768 tokens 104 us, 112 with them in registers)
-  static constexpr bool kPutBy = !BF16 || SHAPE != kPlain;
+  // (bf16 with a cap, 16 x 32768 tokens 110 us; without one, two groups of columns spill 2 registers and four groups 10 where they hold them)
+  static constexpr bool kPutBy = !BF16 || SHAPE != kPlain || CG > 1;
   Columns<BF16, SHAPE, kFewHead> x;
   Seen seen;
 
@@ -464,29 +462,29 @@ struct Wave {
   // What the tokens add to 32 columns of V (REP > 1: to REP groups of them, of which one has this lane's weights).  p * 2^(e - 126): a
   // bf16's bits less 126 - e in its exponent, which are those of a smaller number, and 0 where there would be none; p is up to 2^98.
   template <int X>
-  __device__ __forceinline__ void weigh(const u16x2 (&p)[4][NP][4]) {
+  __device__ __forceinline__ void weigh(const u16x2 (&p)[4][kWeightParts][4]) {
     const u32 times = 0x10001u * (u32)(0x10000 - 128), most = 0x10001u * ((kBias + kFewDown) << 7);
     const u64* from = scales_of(threadIdx.x / kWave) + c * 16 + (X * REP + (REP > 1 ? n / kCols : 0)) * 2;
     const i32x4 scales[2] = {*reinterpret_cast<const i32x4*>(from), *reinterpret_cast<const i32x4*>(from + 8)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {              // eight of the lane's tokens
-      bf16x8 B[NP];
-      u16x2 w[NP][4];
+      bf16x8 B[kWeightParts];
+      u16x2 w[kWeightParts][4];
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         const u32 bytes = __builtin_amdgcn_perm(0, (u32)scales[i >> 1][(i & 1) * 2 + (y >> 1)], y & 1 ? 0x0c030c02 : 0x0c010c00);
         const u16x2 down = mad_pair(bytes, times, most);
 #pragma unroll
-        for (int z = 0; z < NP; ++z) w[z][y] = __builtin_elementwise_sub_sat(p[i][z][y], down);
+        for (int z = 0; z < kWeightParts; ++z) w[z][y] = __builtin_elementwise_sub_sat(p[i][z][y], down);
       }
 #pragma unroll
-      for (int z = 0; z < NP; ++z) B[z] = __builtin_bit_cast(bf16x8, w[z]);
+      for (int z = 0; z < kWeightParts; ++z) B[z] = __builtin_bit_cast(bf16x8, w[z]);
 #pragma unroll
       for (int z = 0; z < 2 * REP; ++z) {
         const int d = X * 2 * REP + z;         // 16 columns
         const bf16x8 A = widen(v[d / 2 * 2 + (i >> 1)][d % 2 * 2 + (i & 1)], 1.f);
 #pragma unroll
-        for (int y = 0; y < NP; ++y) x.o[d] = mfma32(A, B[y], x.o[d]);
+        for (int y = 0; y < kWeightParts; ++y) x.o[d] = mfma32(A, B[y], x.o[d]);
       }
     }
   }
@@ -519,9 +517,9 @@ struct Wave {
         }
         float p[32];
         x.soften(s, scale, p);
-        u16x2 w[4][NP][4];
+        u16x2 w[4][kWeightParts][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) weights<NP>(p + 8 * i, w[i]);
+        for (int i = 0; i < 4; ++i) weights(p + 8 * i, w[i]);
         scales_of(threadIdx.x / kWave)[lane] = vs;
         each_of<kGroups>([&](auto g) { weigh<decltype(g)::value>(w); });
         __builtin_amdgcn_sched_barrier(0);
@@ -802,15 +800,15 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
           for (int j = 0; j < kStageTiles; ++j) gone |= lds.line[stage][j] == kNoTile ? 1u << j : 0u;
           gone = __builtin_amdgcn_readfirstlane(gone);
           const bool hide = base < seen.lo || base + kStageTiles * kTile - 1 > seen.hi || gone;
-          bf16x8 B[NQ][2][NP];
+          bf16x8 B[NQ][2][kWeightParts];
 #pragma unroll
           for (int g = 0; g < NQ; ++g) {
             const float scale = x[g].logits(a, s[g], at);
             if (hide) x[g].hide(s[g], at, [&](int j) { return (gone >> j & 1) != 0; });
             float p[16];
             x[g].soften(s[g], scale, p);
-            parts<NP>(p, B[g][0]);
-            parts<NP>(p + 8, B[g][1]);
+            parts<kWeightParts>(p, B[g][0]);
+            parts<kWeightParts>(p + 8, B[g][1]);
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -818,7 +816,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
 #pragma unroll
             for (int y = 0; y < 4; ++y)
 #pragma unroll
-              for (int p = 0; p < NP; ++p)
+              for (int p = 0; p < kWeightParts; ++p)
 #pragma unroll
                 for (int g = 0; g < NQ; ++g)
                   x[g].o[i % 2 * 4 + y] = mfma32(__builtin_bit_cast(bf16x8, b[i & 1][y]), B[g][i / 2][p], x[g].o[i % 2 * 4 + y]);
