@@ -583,7 +583,7 @@ int kvd_q8_attn(const kvd_q8_cache* cache, const kvd_q8_rows* rows, const void* 
  * first rot_dim elements are turned in pairs by the row's position, and rounded once.
  *   norm (with a weight w): y = x / sqrt(sum x^2 / D + eps) * w;  without: y = x
  *   pair i = elements (i, i + rot_dim/2), or (2i, 2i + 1) if interleaved:  (a, b) -> (a cos t - b sin t, a sin t + b cos t),
- *   t = pos[axis][row] * inv_freq[i], exact to 2^-24 of a turn for positions of any size (products of up to 2^29 turns)
+ *   t = pos[axis][row] * inv_freq[i], exact to 2^-24 of a turn for positions of any size (products of up to 2^50 turns)
  * The pairs are dealt to the axes in order: the first axis_pairs[0] turn by axis 0 and so on (time, height and width of an image's
  * patches; one axis for text).  The sum of squares has to be finite in fp32 (and not below its normal numbers where eps is 0).
  */

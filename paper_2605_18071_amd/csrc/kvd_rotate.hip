@@ -1,6 +1,6 @@
 // Norm and rotation of a step's query and key heads in one pass: y = x / sqrt(mean x^2 + eps) * w, then pairs of elements turned
-// by their position's angle, rounded once.  Angles are revolutions in fp64, position * frequency / 2 pi, of which the fraction
-// is kept: a position beyond 2^20 still has its angle to 2^-26 of a turn.  Bound by the memory, 2 bytes an element read and 2 written:
+// by their position's angle, rounded once.  Angles are turns, position * frequency / 2 pi in twice fp64, of which the fraction is kept.
+// Bound by the memory, 2 bytes an element read and 2 written:
 // 32768 rows of 32 + 8 heads 121 us (5.5 TB/s; a copy of as many bytes takes 130), a step of 64 rows 3.8 (the launch and a trip to memory
 // and back).  Sines are the work of one thread for each pair and row, and shared by the row's heads through LDS; 16 lanes have
 // kAhead heads on their way (154 us with one).
@@ -24,6 +24,14 @@ struct RotateArgs {
   int T, Hq, Hk, pairs, axis_end[4];           // axis_end: first pair behind the axis
   float eps;
 };
+
+// What pos * freq / 2 pi turns have beyond whole ones, off by 2^-25 of a turn at most up to 2^50 turns.  The product has 55 bits, so p and
+// p_rest are all of it, and kPerRadian and kRest are 106 bits of 1 / 2 pi; with 53 of each 5e8 turns were off by 1.5 * 2^-24.
+__device__ __forceinline__ float fraction(int pos, float freq) {
+  constexpr double kPerRadian = 0.15915494309189535, kRest = -9.839338337591243e-18;
+  const double x = (double)pos, f = (double)freq, p = x * f, p_rest = __builtin_fma(x, f, -p);
+  return (float)(__builtin_fma(p, kPerRadian, -rint(p * kPerRadian)) + (p * kRest + p_rest * kPerRadian));
+}
 
 // Cosine and sine of r turns, r in -1/2..1/2: quarter turns taken off, then their series, off by 2^-25 where they end
 __device__ __forceinline__ float2 cos_sin(float r) {
@@ -74,8 +82,7 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_kernel(RotateArgs a) 
     const int r = i / kMaxPairs, p = i % kMaxPairs;
     if (p < a.pairs && row0 + r < a.T) {
       const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
-      const double turns = (double)a.pos[axis * a.pos_stride + row0 + r] * ((double)a.inv_freq[p] * 0.15915494309189533577);
-      turn[r][p] = cos_sin((float)(turns - rint(turns)));
+      turn[r][p] = cos_sin(fraction(a.pos[axis * a.pos_stride + row0 + r], a.inv_freq[p]));
     }
   }
   __syncthreads();
