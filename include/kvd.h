@@ -640,7 +640,8 @@ typedef struct {
   int32_t window;              /* > 0: a row at position p sees tokens from p - window + 1 on */
   const float* slopes;         /* dev [Hq] or NULL: slope * |p - t| is taken off the logit of token t (after the cap) */
   const int32_t* row_from;     /* dev [T] or NULL: first position that a row sees (its document's first token) */
-  const int32_t* prefix_len;   /* dev [B] or NULL: every row of the sequence sees its first prefix_len tokens, later ones than itself too */
+  const int32_t* prefix_len;   /* dev [B] or NULL: every row of the sequence sees on to its first prefix_len tokens' end, later ones than
+                                  itself too.  Only to that side: window and row_from hide tokens of the prefix as they do others */
 } kvd_q4_scores;
 
 /* Quantises the step's keys and values into their pages, run by run and head by head; arguments as for kvd_q8_append.
