@@ -65,7 +65,7 @@ class Step:
         self.cache.attend(self.rows, q, out, self.cache.workspace(self.rows) if ws is None else ws, lse=ls, stream=stream, **kw)
         return out, ls
 
-    def check(self, q, out, lse, *, rows=None, table=None, softcap=0.0, window=0, slopes=None, row_from=None, prefix_len=None):
+    def check(self, q, out, lse, *, rows=None, table=None, softcap=0.0, window=0, slopes=None, row_from=None, prefix_len=None, weights=None):
         """Rows against the 64-bit definition.  With A = sum p |v| / sum p, an output is off by at most
            half a step of its type                                                                     h |o|
          + the weights' rounding to bf16, half a step of 8 bits: 2^-8 (f16: the rest's, 2^-16)         r A
@@ -73,11 +73,12 @@ class Step:
          + what fp32 cannot hold: weights times scales are kept with the row's largest weight at 2^-36, and what is below fp32's least
            normal 2^-126 may be lost: 2^(36 - 126) of a code of up to 6 for each token                            n 2^-87
          + f16: below its normal numbers                                                               2^-25.
+        `weights`: r, where that has to be less.
         Logits: products of 128 elements and their sums in fp32 (2^-17 sum |q k| scale), a cap's exponent and reciprocal (2^-20 of the
         cap; above 64 of the logit), a bias's rounding (2^-22), the exponent's argument (2^-23 of it) and 2^-20."""
         ref, table = self.ref(), self.table if table is None else table
         h = torch.finfo(torch_type(self.dtype)).eps / 2
-        r = 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -16
+        r = weights or (2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -16)
         scale = self.scale or 1.0 / math.sqrt(D)
         qd, od, ld = q.double().cpu().numpy(), out.double().cpu().numpy(), None if lse is None else lse.double().cpu().numpy()
         sl = None if slopes is None else np.asarray(slopes, dtype=np.float64)
