@@ -69,7 +69,7 @@ __device__ __forceinline__ void each_of(F f) {
     f(std::integral_constant<int, N - 1>{});
   }
 }
-template <bool ONCE>                           // whether nobody else reads them
+template <bool ONCE>                           // whether no other wave of the workgroup reads them
 __device__ __forceinline__ i32x4 load_codes(const unsigned char* p) {
   if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p));
   else return *reinterpret_cast<const i32x4*>(p);
