@@ -144,7 +144,8 @@ __device__ __forceinline__ u32 widen2(u32 codes, float scale) {
 
 // Keys lie in the order of their elements: 16 lanes have a token, four tokens at a time.  Values lie by element, all tokens of a tile in
 // 8 bytes: neighbouring lanes exchange theirs, so that each has two elements that follow each other, and 64 lanes write a
-// token whole.  Rows that follow each other in a tile take it together; any others have a turn of their own.
+// token whole.  Rows that follow each other in a tile take it together; any others have a turn of their own, and a trip to memory in it: 64 rows of
+// one sequence 5.7 us, of as many sequences 11.1; 16384 rows in pieces 15, by chance 39.
 // HP heads have their rows looked up once, and are on their way together.  Bound by the memory: 20 k tokens of 8 heads to f16 18.6 us (5.6
 // TB/s), 300 tokens 6.0 (rows, table, tile: three trips one behind the other).
 template <bool BF16, int HP>

@@ -31,10 +31,10 @@ constexpr int kAttnGroups = 512;               // workgroups: two for each CU
 constexpr int kStep = 8;                       // tiles that a wave takes at a time
 constexpr int kLeastTiles = 32;                // tiles of a workgroup at least
 // What a unit costs whatever its length, in tiles: without it the workgroups that have many short units come last (2 x 4096 rows from
-// the start 433 us for 343, 24 drafts of ragged contexts 137 for 131)
+// the start 510 us for 440, 24 drafts of ragged contexts 118 for 116)
 constexpr int kFewPad = 16, kRowsPad = 24;
-// Tiles of a workgroup where there are few, so that most units need no joining: 30 x 3000 tokens of 8 heads 20 us; with 32 26, with 128
-// 25.  4 x 2500: 13.3, 12.8, 16.0
+// Tiles of a workgroup where there are few, so that most units need no joining: 30 contexts of up to 3000 tokens of 8 heads 22 us; with 32
+// 28, with 128 27.  4 x 2500: 14.9, 14.0, 18.2
 constexpr int kPieceTiles = 64;
 // What becomes of logits, in kernels of their own (a branch for large caps in the ones without: f16 drafts 136 us for 123)
 constexpr int kPlain = 0, kShaped = 1, kShapedFar = 2;         // nothing; a cap, slopes; a cap above kNearCap, slopes
@@ -348,10 +348,11 @@ __device__ __forceinline__ const unsigned char* tile_at(const AttnArgs& a, u32 l
 // second product sums over: they go into the weights, so that each group of 32 columns of V has weights of its own, p * 2^e.  Where
 // columns would be empty they repeat the rows (REP): each copy weighs the values of a fraction of the groups.  CG waves share tokens
 // and have 16 columns each.
-// One row a sequence is bound by the memory: 16 x 32768 tokens of 8 heads 99 us (5.8 TB/s); 4 x 1000 tokens 10.9 us by its chain of trips
-// to memory.  More columns are bound by the vector unit's instructions, some 480 to 1100 for 128 tokens of a wave, which two waves a SIMD
-// issue one each 4.5 cycles: 24 ragged contexts with up to 3 rows of 7 x 4 heads, f16, capped and sloped, 121 us (2.4 TB/s), 64 for one
-// row in bf16.  (64 tokens at a time and three waves a SIMD: 117 us for 99, as each step has as much around it.)
+// One row a sequence is bound by the memory: 16 x 32768 tokens of 8 heads 101 to 105 us (5.5 TB/s), f16 107; 4 contexts of up to 1000 tokens
+// 11.9 us by their chain of trips to memory.  More columns are bound by the vector unit's instructions, some 580 to 1100 for 128 tokens of a wave,
+// which two waves a SIMD issue one each 4.5 cycles: 24 ragged contexts with up to 3 rows of 7 x 4 heads, f16, capped and sloped, 116 us (2.5
+// TB/s), 64 for one row in bf16.  (With one part of weights, 64 tokens at a time and three waves a SIMD: 117 us for 99, as each step has as
+// much around it.)
 // What a lane would not need all the time lies in LDS, its wave's scales of values and, where registers are short, its queries: spilled
 // ones came back behind the loads on their way, and the wait for them was one for all of those (the drafts 133 us, with the queries
 // alone in LDS 126).
@@ -671,9 +672,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void q4_attn_kernel(AttnArgs a) {
 // Each wave has its own kRowGroups * 16 columns, and the workgroup's WAVES go through the tokens together, 64 at a time: waves fetch a
 // tile each, widen it and put it into LDS in operand order, while the 64 before it are taken; so a code is widened once for all
 // of them.  Values take their scales there.  Of eight waves four have the keys and four the values.
-// Bound by issue: about 330 vector instructions, 64 products and 33 trips to LDS a wave and stage, two waves a SIMD, vector unit and
-// matrix cores busy 55 % and 30 % of the time.  2 x 2048 rows of 32/8 heads behind 6144 tokens 510 us (940 TFLOP/s), in documents of
-// 5000 tokens 208 (700), 2 x 4096 rows from the start 340 (810).  (32 x 32 products: 229 for 210, as only two chains of them go at a time.)
+// Bound by issue and by phases that all waves are in at once: about 410 vector instructions, 96 products (a third of them for the
+// second part of the weights) and 33 trips to LDS a wave and stage, two waves a SIMD, vector unit and matrix cores busy 55 % and 40 to 45 %
+// of the time.  2 x 2048 rows of 32/8 heads behind 6144 tokens 668 us (720 TFLOP/s without the second part's), in documents of 5000 tokens
+// 245 to 260 (580), 2 x 4096 rows from the start 440 (630); the documents in f16 309, with a cap 296, with slopes too 342, f16 374.  (With
+// one part of weights 32 x 32 products took 229 us for 210, as only two chains of them go at a time.)
 constexpr int kRowGroups = 2;
 constexpr int kStageTiles = 4;
 template <int WAVES>
@@ -871,9 +874,11 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void q4_attn_rows_kernel(AttnArgs 
 }
 
 // How the columns that the rows of a sequence take, on the average, are laid out: copies of them in 16, or groups of 16 (0: workgroups
-// of 4 or 8 waves with rows of their own).  us: 30 x up to 3000 tokens, 4 columns: four copies 20.5, one 21.1.  16 x 6000 tokens of 8
-// heads, 64 columns: four groups 69, 4 waves with rows 84; 96: 106, 91; 128: 113, 95, and 8 waves with rows 104; 160: 4 waves 144, 8
-// waves 127; 252: 149, 142.
+// of 4 or 8 waves with rows of their own).  us: 30 x up to 3000 tokens, 4 columns: four copies 21.7, one 22.1.  16 x 6000 tokens of 8
+// heads, 64 columns: four groups 85, 4 waves with rows 103; 96: 125, 107; 128: 130, 112, and 8 waves with rows 120; 160: 4 waves 171, 8
+// waves 162; 252: 181, 183.  All sequences of a step have one layout, which is right for those that are alike: 63 single tokens
+// behind 32768 take 389 us and 2048 rows behind 6144 368, but a step of all of them 3267, its single tokens in waves with rows (with
+// 512 rows 114, and 1101 together, those rows in units of 16 columns).
 struct Shape { int copies, groups, waves; };
 static Shape shape_of(int T, int B, int G) {
   const int64_t want = (int64_t)((T + B - 1) / B) * G;
