@@ -665,8 +665,8 @@ int64_t kvd_q4_workspace_bytes(const kvd_q4_cache* cache, const kvd_q8_rows* row
  *   q [T][Hq][D] kv_dtype, rows q_stride elements apart;  out [T][Hq][D] kv_dtype;  lse [T][Hq] fp32 or NULL.
  * out = softmax(f(scale * q K^T)) V, lse = log sum exp of the logits; 0 and -infinity where a row sees nothing.  Sums, maxima and
  * accumulators are fp32; the weights that multiply V have 16 bits (off by 2^-16 of themselves at most).  Relative to the row's largest
- * weight, a weight times its value's scale has fewer bits below 2^-74 and is lost below 2^-90.  A capped logit is off by 2^-20 of the cap at
- * most, or of itself where the cap is above 64.  The products q K^T of what a row sees, and its logits, have to be finite in fp32; a row
+ * weight, a weight, and a weight times its value's scale, has fewer bits below 2^-74 and is lost below 2^-90.  A capped logit is off by
+ * 2^-20 of the cap at most, or of itself where the cap is above 64.  The products q K^T of what a row sees, and its logits, have to be finite in fp32; a row
  * and head with a query that is not finite gives NaN.  Rows without a sequence are left as they were.  kv_len and row_start must be
  * those of row_seq and row_pos. */
 int kvd_q4_attn(const kvd_q4_cache* cache, const kvd_q8_rows* rows, const void* q, int64_t q_stride, const kvd_q4_scores* scores,
